@@ -64,6 +64,8 @@ typedef enum {
 /* Bits of the `flags` argument of the convolution entry points. */
 #define ALCS_RELU 1u            /* y = max(acc + bias, 0)                                           */
 #define ALCS_Y_F32 2u           /* 16-bit weights only: write Y (and read a residual) as fp32 instead of the 16-bit type */
+/* alcs_group_norm and its backward pass only: ALCS_RELU or this one.                                */
+#define ALCS_SILU 4u            /* y = z / (1 + exp(-z))                                             */
 
 typedef struct alcs_packed alcs_packed;   /* opaque packed weight matrix, library-owned */
 typedef struct alcs_stack alcs_stack;     /* opaque layer stack, library-owned          */
@@ -445,6 +447,86 @@ ALCS_API int alcs_spconv2d_cfg(const alcs_packed* w, const void* x, void* y, int
                                const alcs_conv2d_cfg* cfg, void* cuda_stream);
 ALCS_API int alcs_spconv2d_plan(const alcs_packed* w, int n, int cin, int h, int wd, int kh, int kw,
                                 int stride, int pad, alcs_conv2d_cfg* out);
+
+/* ---------------------------------------------------------------------------------------------
+ * Group norm with an activation, channels last (device).
+ *
+ * The layer between two pointwise layers, for inference and for the fine-tuning that follows pruning.  The `c` channels are
+ * `groups` groups of c / groups neighbours; over the pixels and channels of a group of an image
+ *     mu = mean x,  var = mean (x - mu)^2,  rstd = 1 / sqrt(var + eps),  xh = (x - mu) * rstd,
+ *     z = gamma[channel] * xh + beta[channel],  y = act(z),  act the identity, ALCS_RELU or ALCS_SILU (flags).
+ * x and y are device [n][h*wd][c] (NHWC), contiguous, of type dt, aligned to their element size; y may be x itself, but not
+ * overlap it otherwise.  gamma and beta are device fp32 [c] or NULL (1 and 0); mean and rstd receive mu and rstd, device fp32
+ * [n][groups], or are NULL.  Statistics and everything up to the rounding of y are fp32; the variance is that of values with
+ * their mean (of the part of the group a thread block has) taken off, so that a mean far from 0 costs no accuracy.  An infinity
+ * or NaN makes its group of its image NaN.  ReLU turns NaN into 0, as in the convolutions.
+ *
+ * alcs_group_norm_backward: for the derivative dy of a loss by y, with dz = dy * act'(z) (act' of ReLU at 0 is 0) and t = gamma * dz,
+ *     dbeta = sum dz,  dgamma = sum dz * xh  (over images and pixels),
+ *     dx = rstd * (t - mean t - xh * mean (t * xh))  (means over the group).
+ * mean and rstd are what alcs_group_norm stored for the same x; dy and dx are like x, dx may be dy or x itself; dgamma and
+ * dbeta are device fp32 [c] or NULL, and are overwritten.  The order of all sums is fixed: the same call gives the same bits.
+ *
+ * workspace: device memory of at least alcs_group_norm_workspace() bytes, 16-byte aligned, for either call (the forward
+ * pass needs it where a group's part of an image is spread over more thread blocks than can exchange sums directly; NULL and 0 where
+ * that function says 0).  Its content matters only within a call; calls that may overlap on the GPU need one each, and so do
+ * captured graphs that may.
+ * All buffers belong to the current device.  One to four kernels on cuda_stream; no allocation, no synchronisation.  n == 0 or
+ * h*wd == 0 is a successful no-op, but for dgamma and dbeta, which become 0.
+ * Errors: INVALID_ARG (null, misaligned or overlapping buffers, host memory, negative sizes, groups < 1, an eps that is negative or not finite, both
+ * activations, workspace too small), SHAPE (c not a multiple of groups, h*wd or n*c of 2^30 and more, c above 65536),
+ * STATE (memory of another device), CUDA.
+ * ------------------------------------------------------------------------------------------- */
+ALCS_API size_t alcs_group_norm_workspace(int n, int h, int wd, int c, int groups, alcs_dtype dt);
+ALCS_API int alcs_group_norm(const void* x, void* y, int n, int h, int wd, int c, int groups, const float* gamma, const float* beta,
+                             float eps, unsigned flags, alcs_dtype dt, float* mean, float* rstd, void* workspace,
+                             size_t workspace_bytes, void* cuda_stream);
+ALCS_API int alcs_group_norm_backward(const void* x, const void* dy, void* dx, int n, int h, int wd, int c, int groups,
+                                      const float* mean, const float* rstd, const float* gamma, const float* beta, float* dgamma,
+                                      float* dbeta, unsigned flags, alcs_dtype dt, void* workspace, size_t workspace_bytes,
+                                      void* cuda_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Microscaled 4-bit floating point: the other way of making a pointwise layer small (device).
+ *
+ * Format (MXFP4 of the OCP Microscaling Formats specification 1.0): 32 consecutive values of a row share one scale,
+ * 2^(s - 127) for a byte s in 0 .. 254 (255: the block is NaN); a value is 4 bits, E2M1: sign, two bits of exponent, one of
+ * mantissa, i.e. one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Storage of a matrix [rows][cols], in the order in which the tensor cores read it,
+ * so that a tile of 128 rows is fetched by copies of whole runs of memory:
+ *     data    [ceil(rows/128)][2 * ceil(cols/64)][128][16]   tile of rows, block of 32 columns, row, byte; byte j of a block holds
+ *                                                            its value 2j in the low and 2j + 1 in the high four bits
+ *     scales  [ceil(rows/128)][ceil(cols/128)][32][4][4]     tile of rows, group of four blocks, row % 32, row / 32 % 4, block % 4
+ * Values behind the last column, and an odd last block's neighbour, have code 0 and any scale but 255; rows behind the last
+ * may hold anything, are never read into a result and never written.  alcs_mx4_bytes gives the sizes of both arrays (host only).
+ *
+ * alcs_mx4_quantize: x device [rows] rows of cols values of type dt, ldx (>= cols) elements apart.  Per block, with m the
+ * largest magnitude: s - 127 = max(floor(log2 m) - 2, -127) (m = 0: -127), values are divided by the scale, exactly, and
+ * rounded to the nearest code, ties to even mantissa, magnitudes above 6 to 6; a zero keeps its sign.  A block with an infinity or NaN
+ * gets s = 255.  alcs_mx4_dequantize: the values as type dt (one rounding; NaN for s = 255), y rows ldy elements apart; what lies between
+ * its rows is left alone.
+ *
+ * alcs_mx4_product: y[r][o] = act( sum_c x[r][c] * w[o][c] + bias[o] + residual[r][o] ): a pointwise layer on channels-last
+ * pixels, or any linear layer.  x is [rows][cin] and w [cout][cin] in the format above; y and residual are device [rows][cout], contiguous, of
+ * type dt; bias device fp32 [cout] or NULL, residual may be NULL or y itself; flags = ALCS_RELU or 0 (which turns NaN into 0).  On the
+ * fifth-generation tensor cores, fp32 accumulation, one rounding; one kernel, no allocation, no synchronisation, the same bits every time.
+ * A NaN block makes its row (of x) or column (of w) of y NaN, before the activation.  cin == 0 gives act(bias + residual).
+ *
+ * data and scales are 16-byte aligned, x and y to their element size.  All buffers belong to the current device.  rows == 0 (cols == 0, cout == 0)
+ * is a successful no-op.
+ * Errors: INVALID_ARG (null, misaligned or overlapping buffers, host memory, negative sizes, ld < cols, unknown flags or types), SHAPE (rows
+ * or columns beyond 2^30, cin or cols beyond 2^24, more than 2^31 - 1 tiles of y), STATE (memory of another device), CUDA.
+ * ------------------------------------------------------------------------------------------- */
+ALCS_API int alcs_mx4_bytes(int rows, int cols, size_t* data_bytes, size_t* scale_bytes);
+ALCS_API int alcs_mx4_quantize(const void* x, int rows, int cols, long long ldx, alcs_dtype dt, void* data, void* scales, void* cuda_stream);
+ALCS_API int alcs_mx4_dequantize(const void* data, const void* scales, int rows, int cols, void* y, long long ldy, alcs_dtype dt,
+                                 void* cuda_stream);
+ALCS_API int alcs_mx4_product(const void* x, const void* x_scales, int rows, const void* w, const void* w_scales, int cout, int cin,
+                              void* y, const float* bias, const void* residual, unsigned flags, alcs_dtype dt, void* cuda_stream);
+/*
+ * alcs_mx4_status: the error word of the current device's alcs_mx4_product calls (synchronises with the device).  *code is 0 unless a
+ * kernel gave up one of its bounded waits: 1 = for data, 2 = for a free pipeline stage; the outputs of that launch are then incomplete.
+ */
+ALCS_API int alcs_mx4_status(int* code);
 
 /* ---------------------------------------------------------------------------------------------
  * Latency model and projection with bisection.

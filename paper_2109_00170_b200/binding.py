@@ -19,7 +19,7 @@ ALCS_ERR_INVALID_ARG, ALCS_ERR_SHAPE, ALCS_ERR_UNSUPPORTED, ALCS_ERR_ALLOC = -1,
 ALCS_ERR_CUDA, ALCS_ERR_CORRUPT, ALCS_ERR_STATE, ALCS_ERR_TOO_LARGE = -5, -6, -7, -8
 ALCS_NOALLOC_SCRATCH_BYTES = 16 << 20
 ALCS_F32, ALCS_F16, ALCS_BF16 = 0, 1, 2
-ALCS_RELU, ALCS_Y_F32 = 1, 2
+ALCS_RELU, ALCS_Y_F32, ALCS_SILU = 1, 2, 4
 ALCS_STACK_GRAPH = 1
 
 # every symbol include/alcs.h declares
@@ -29,7 +29,8 @@ EXPORTS = ["alcs_strerror", "alcs_last_cuda_error", "alcs_version", "alcs_pack",
            "alcs_variant_count", "alcs_variant_get",
            "alcs_spconv1x1", "alcs_spconv1x1_cfg", "alcs_spconv1x1_ex",
            "alcs_spconv1x1_plan", "alcs_spconv1x1_tune", "alcs_spconv1x1_set_cfg", "alcs_spconv1x1_host_workspace",
-           "alcs_spconv1x1_host", "alcs_spconv1x1_noalloc", "alcs_spconv2d", "alcs_spconv2d_cfg", "alcs_spconv2d_plan", "alcs_layer_latency", "alcs_network_latency",
+           "alcs_spconv1x1_host", "alcs_spconv1x1_noalloc", "alcs_spconv2d", "alcs_spconv2d_cfg", "alcs_spconv2d_plan", "alcs_group_norm_workspace", "alcs_group_norm",
+           "alcs_group_norm_backward", "alcs_mx4_bytes", "alcs_mx4_quantize", "alcs_mx4_dequantize", "alcs_mx4_product", "alcs_mx4_status", "alcs_layer_latency", "alcs_network_latency",
            "alcs_project_bisection", "alcs_probe_fma_peak", "alcs_probe_lds", "alcs_probe_segment_loop",
            "alcs_stack_create", "alcs_stack_run", "alcs_stack_destroy", "alcs_stack_tune", "alcs_stack_layer_cfg"]
 
@@ -135,6 +136,16 @@ def lib():
     L.alcs_spconv2d.argtypes = [vp, vp, vp] + [i] * 8 + [vp, u, vp]
     L.alcs_spconv2d_cfg.argtypes = [vp, vp, vp] + [i] * 8 + [vp, u, C.POINTER(Conv2dCfg), vp]
     L.alcs_spconv2d_plan.argtypes = [vp] + [i] * 8 + [C.POINTER(Conv2dCfg)]
+    f, ll = C.c_float, C.c_longlong
+    L.alcs_group_norm_workspace.argtypes = [i] * 6
+    L.alcs_group_norm_workspace.restype = sz
+    L.alcs_group_norm.argtypes = [vp, vp] + [i] * 5 + [vp, vp, f, u, i, vp, vp, vp, sz, vp]
+    L.alcs_group_norm_backward.argtypes = [vp] * 3 + [i] * 5 + [vp] * 6 + [u, i, vp, sz, vp]
+    L.alcs_mx4_bytes.argtypes = [i, i, C.POINTER(sz), C.POINTER(sz)]
+    L.alcs_mx4_quantize.argtypes = [vp, i, i, ll, i, vp, vp, vp]
+    L.alcs_mx4_dequantize.argtypes = [vp, vp, i, i, vp, ll, i, vp]
+    L.alcs_mx4_product.argtypes = [vp, vp, i, vp, vp, i, i, vp, vp, vp, u, i, vp]
+    L.alcs_mx4_status.argtypes = [ip]
     L.alcs_layer_latency.argtypes = [C.POINTER(LatencyTable), C.c_int64, C.POINTER(C.c_double)]
     L.alcs_network_latency.argtypes = [C.c_double, C.POINTER(LatencyTable), i, C.POINTER(C.c_int64), C.POINTER(C.c_double)]
     L.alcs_project_bisection.argtypes = [C.POINTER(vp), ip, ip, i, i, C.POINTER(LatencyTable), C.c_double, C.c_double,
@@ -412,6 +423,58 @@ def alcs_spconv2d_plan(w: Packed, n: int, cin: int, h: int, wd: int, kh: int, kw
     _check(lib().alcs_spconv2d_plan(w.handle, n, cin, h, wd, kh, kw, stride, pad, C.byref(out)),
            "alcs_spconv2d_plan")
     return out.as_dict()
+
+
+def alcs_group_norm_workspace(n: int, h: int, wd: int, c: int, groups: int, dt: int = ALCS_F32) -> int:
+    """Bytes of workspace that either call of group norm needs at this shape."""
+    return int(lib().alcs_group_norm_workspace(n, h, wd, c, groups, dt))
+
+
+def alcs_group_norm(x, y, n: int, h: int, wd: int, c: int, groups: int, gamma=None, beta=None, eps: float = 1e-5, flags: int = 0,
+                    dt: int = ALCS_F32, mean=None, rstd=None, workspace=None, workspace_bytes: int = 0, stream=None):
+    """y = act(group norm of x), channels last: x, y [n, h, wd, c] of type dt; mean, rstd [n, groups] fp32 where the
+    backward pass will need them."""
+    _check(lib().alcs_group_norm(_addr(x), _addr(y), n, h, wd, c, groups, _addr(gamma), _addr(beta), eps, flags, dt, _addr(mean),
+                                 _addr(rstd), _addr(workspace), workspace_bytes, _stream(stream)), "alcs_group_norm")
+
+
+def alcs_group_norm_backward(x, dy, dx, n: int, h: int, wd: int, c: int, groups: int, mean, rstd, gamma=None, beta=None, dgamma=None,
+                             dbeta=None, flags: int = 0, dt: int = ALCS_F32, workspace=None, workspace_bytes: int = 0, stream=None):
+    """dx, dgamma and dbeta of alcs_group_norm for the derivative dy by its output; mean, rstd as that call stored them."""
+    _check(lib().alcs_group_norm_backward(_addr(x), _addr(dy), _addr(dx), n, h, wd, c, groups, _addr(mean), _addr(rstd), _addr(gamma),
+                                          _addr(beta), _addr(dgamma), _addr(dbeta), flags, dt, _addr(workspace), workspace_bytes,
+                                          _stream(stream)), "alcs_group_norm_backward")
+
+
+def alcs_mx4_bytes(rows: int, cols: int):
+    """Bytes of the data and of the scales of a microscaled 4-bit matrix."""
+    d, s = C.c_size_t(), C.c_size_t()
+    _check(lib().alcs_mx4_bytes(rows, cols, C.byref(d), C.byref(s)), "alcs_mx4_bytes")
+    return d.value, s.value
+
+
+def alcs_mx4_quantize(x, rows: int, cols: int, ldx: int, dt: int, data, scales, stream=None):
+    """x: `rows` rows of `cols` values of type dt, ldx elements apart, to microscaled 4-bit floating point."""
+    _check(lib().alcs_mx4_quantize(_addr(x), rows, cols, ldx, dt, _addr(data), _addr(scales), _stream(stream)), "alcs_mx4_quantize")
+
+
+def alcs_mx4_dequantize(data, scales, rows: int, cols: int, y, ldy: int, dt: int, stream=None):
+    """The values of a microscaled 4-bit matrix, as type dt, rows ldy elements apart."""
+    _check(lib().alcs_mx4_dequantize(_addr(data), _addr(scales), rows, cols, _addr(y), ldy, dt, _stream(stream)), "alcs_mx4_dequantize")
+
+
+def alcs_mx4_product(x, x_scales, rows: int, w, w_scales, cout: int, cin: int, y, bias=None, residual=None, flags: int = 0,
+                     dt: int = ALCS_F32, stream=None):
+    """y = act(x w^T + bias + residual) of two microscaled 4-bit matrices x [rows, cin], w [cout, cin]; y [rows, cout] of type dt."""
+    _check(lib().alcs_mx4_product(_addr(x), _addr(x_scales), rows, _addr(w), _addr(w_scales), cout, cin, _addr(y), _addr(bias),
+                                  _addr(residual), flags, dt, _stream(stream)), "alcs_mx4_product")
+
+
+def alcs_mx4_status() -> int:
+    """Error word of the current device's products: 0 unless a kernel gave up a bounded wait."""
+    code = C.c_int(0)
+    _check(lib().alcs_mx4_status(code), "alcs_mx4_status")
+    return code.value
 
 
 _TABLE_DTYPE = np.dtype([("n", np.int32), ("pad", np.int32), ("k", np.uintp), ("t", np.uintp)])

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import concurrent.futures as cf
 import os
+import re
 import shutil
 import subprocess
 import sys
@@ -23,9 +24,9 @@ LIB = os.path.join(PKG, "libalcs.so")
 # The binding's most frequent calls, marshalled in C; the name carries the Python it is for, so that no other one loads it.
 CALL = os.path.join(PKG, "_alcs_call" + sysconfig.get_config_var("EXT_SUFFIX"))
 
-SOURCES = ["alcs_pack.cpp", "alcs_device.cu", "alcs_conv2d.cu", "alcs_project.cu", "alcs_gather.cu", "alcs_probe.cu", "alcs_tc.cu", "alcs_tc16.cu", "alcs_tc_prep.cu", "alcs_variants_f32_g4.cu",
+SOURCES = ["alcs_pack.cpp", "alcs_device.cu", "alcs_conv2d.cu", "alcs_project.cu", "alcs_gather.cu", "alcs_probe.cu", "alcs_tc.cu", "alcs_tc16.cu", "alcs_tc_prep.cu", "alcs_norm.cu", "alcs_mx4.cu", "alcs_mx4_product.cu", "alcs_variants_f32_g4.cu",
            "alcs_variants_f32_other.cu", "alcs_variants_f16.cu", "alcs_variants_f16_mma.cu", "alcs_variants_bf16.cu"]
-HEADERS = ["alcs_internal.h", "alcs_kernels.cuh", "alcs_mma.cuh", "alcs_conv2d.cuh", "alcs_gather.h", "alcs_tc.h", "alcs_tc.cuh", "alcs_tc_prep.h"]
+HEADERS = ["alcs_internal.h", "alcs_kernels.cuh", "alcs_mma.cuh", "alcs_conv2d.cuh", "alcs_gather.h", "alcs_tc.h", "alcs_tc.cuh", "alcs_tc_prep.h", "alcs_dense.h"]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC,-Wall,-fvisibility=hidden", "-I", os.path.join(ROOT, "include"),
@@ -45,13 +46,23 @@ def _newest_dep() -> float:
     return max(os.path.getmtime(d) for d in deps)
 
 
+def _included(name: str, seen: set) -> set:
+    """The sources and headers that compiling `name` reads, of this repository's."""
+    if name not in seen:
+        seen.add(name)
+        path = os.path.join(CSRC, name)
+        with open(path if os.path.exists(path) else os.path.join(ROOT, "include", name)) as f:
+            for h in re.findall(r'^\s*#\s*include\s+"([^"]+)"', f.read(), re.M):
+                _included(h, seen)
+    return seen
+
+
 def _compile(src: str, verbose: bool) -> str:
     obj = os.path.join(OBJ, os.path.splitext(src)[0] + ".o")
     srcp = os.path.join(CSRC, src)
-    hdr_time = max(os.path.getmtime(os.path.join(CSRC, h)) for h in HEADERS)
-    hdr_time = max(hdr_time, os.path.getmtime(os.path.join(ROOT, "include", "alcs.h")),
-                   os.path.getmtime(os.path.abspath(__file__)))
-    if os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(srcp), hdr_time):
+    paths = [os.path.join(CSRC, h) for h in _included(src, set()) if h != "alcs.h"]
+    newest = max(os.path.getmtime(p) for p in paths + [os.path.join(ROOT, "include", "alcs.h"), os.path.abspath(__file__)])
+    if os.path.exists(obj) and os.path.getmtime(obj) >= newest:
         return obj
     cmd = [_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-x", "cu", "-c", srcp, "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
