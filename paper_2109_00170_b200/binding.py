@@ -35,6 +35,10 @@ EXPORTS = ["alcs_strerror", "alcs_last_cuda_error", "alcs_version", "alcs_pack",
            "alcs_stack_create", "alcs_stack_run", "alcs_stack_destroy", "alcs_stack_tune", "alcs_stack_layer_cfg"]
 
 
+# of them, those that _alcs_call's bind_dense takes, in its order
+DENSE = ("alcs_group_norm", "alcs_group_norm_backward", "alcs_mx4_quantize", "alcs_mx4_dequantize", "alcs_mx4_product")
+
+
 class AlcsError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -96,6 +100,7 @@ class _NoCall:
         return None
 
     spconv1x1 = spconv1x1_ex = spconv2d = stack_run = _none
+    group_norm = group_norm_backward = mx4_quantize = mx4_dequantize = mx4_product = _none
 
 
 def lib():
@@ -166,6 +171,7 @@ def lib():
     try:
         from . import _alcs_call as native
         native.bind(*(C.cast(getattr(L, name), vp).value for name in ("alcs_spconv1x1", "alcs_spconv1x1_ex", "alcs_spconv2d", "alcs_stack_run")))
+        native.bind_dense(*(C.cast(getattr(L, name), vp).value for name in DENSE))
     except ImportError:
         native = _NoCall
     _lib, _call = L, native
@@ -434,16 +440,25 @@ def alcs_group_norm(x, y, n: int, h: int, wd: int, c: int, groups: int, gamma=No
                     dt: int = ALCS_F32, mean=None, rstd=None, workspace=None, workspace_bytes: int = 0, stream=None):
     """y = act(group norm of x), channels last: x, y [n, h, wd, c] of type dt; mean, rstd [n, groups] fp32 where the
     backward pass will need them."""
-    _check(lib().alcs_group_norm(_addr(x), _addr(y), n, h, wd, c, groups, _addr(gamma), _addr(beta), eps, flags, dt, _addr(mean),
-                                 _addr(rstd), _addr(workspace), workspace_bytes, _stream(stream)), "alcs_group_norm")
+    st = _native().group_norm(x, y, n, h, wd, c, groups, gamma, beta, eps, flags, dt, mean, rstd, workspace, workspace_bytes, stream)
+    if st is None:
+        st = lib().alcs_group_norm(_addr(x), _addr(y), n, h, wd, c, groups, _addr(gamma), _addr(beta), eps, flags, dt, _addr(mean),
+                                   _addr(rstd), _addr(workspace), workspace_bytes, _stream(stream))
+    if st != ALCS_OK:
+        _check(st, "alcs_group_norm")
 
 
 def alcs_group_norm_backward(x, dy, dx, n: int, h: int, wd: int, c: int, groups: int, mean, rstd, gamma=None, beta=None, dgamma=None,
                              dbeta=None, flags: int = 0, dt: int = ALCS_F32, workspace=None, workspace_bytes: int = 0, stream=None):
     """dx, dgamma and dbeta of alcs_group_norm for the derivative dy by its output; mean, rstd as that call stored them."""
-    _check(lib().alcs_group_norm_backward(_addr(x), _addr(dy), _addr(dx), n, h, wd, c, groups, _addr(mean), _addr(rstd), _addr(gamma),
-                                          _addr(beta), _addr(dgamma), _addr(dbeta), flags, dt, _addr(workspace), workspace_bytes,
-                                          _stream(stream)), "alcs_group_norm_backward")
+    st = _native().group_norm_backward(x, dy, dx, n, h, wd, c, groups, mean, rstd, gamma, beta, dgamma, dbeta, flags, dt, workspace,
+                                       workspace_bytes, stream)
+    if st is None:
+        st = lib().alcs_group_norm_backward(_addr(x), _addr(dy), _addr(dx), n, h, wd, c, groups, _addr(mean), _addr(rstd), _addr(gamma),
+                                            _addr(beta), _addr(dgamma), _addr(dbeta), flags, dt, _addr(workspace), workspace_bytes,
+                                            _stream(stream))
+    if st != ALCS_OK:
+        _check(st, "alcs_group_norm_backward")
 
 
 def alcs_mx4_bytes(rows: int, cols: int):
@@ -455,19 +470,31 @@ def alcs_mx4_bytes(rows: int, cols: int):
 
 def alcs_mx4_quantize(x, rows: int, cols: int, ldx: int, dt: int, data, scales, stream=None):
     """x: `rows` rows of `cols` values of type dt, ldx elements apart, to microscaled 4-bit floating point."""
-    _check(lib().alcs_mx4_quantize(_addr(x), rows, cols, ldx, dt, _addr(data), _addr(scales), _stream(stream)), "alcs_mx4_quantize")
+    st = _native().mx4_quantize(x, rows, cols, ldx, dt, data, scales, stream)
+    if st is None:
+        st = lib().alcs_mx4_quantize(_addr(x), rows, cols, ldx, dt, _addr(data), _addr(scales), _stream(stream))
+    if st != ALCS_OK:
+        _check(st, "alcs_mx4_quantize")
 
 
 def alcs_mx4_dequantize(data, scales, rows: int, cols: int, y, ldy: int, dt: int, stream=None):
     """The values of a microscaled 4-bit matrix, as type dt, rows ldy elements apart."""
-    _check(lib().alcs_mx4_dequantize(_addr(data), _addr(scales), rows, cols, _addr(y), ldy, dt, _stream(stream)), "alcs_mx4_dequantize")
+    st = _native().mx4_dequantize(data, scales, rows, cols, y, ldy, dt, stream)
+    if st is None:
+        st = lib().alcs_mx4_dequantize(_addr(data), _addr(scales), rows, cols, _addr(y), ldy, dt, _stream(stream))
+    if st != ALCS_OK:
+        _check(st, "alcs_mx4_dequantize")
 
 
 def alcs_mx4_product(x, x_scales, rows: int, w, w_scales, cout: int, cin: int, y, bias=None, residual=None, flags: int = 0,
                      dt: int = ALCS_F32, stream=None):
     """y = act(x w^T + bias + residual) of two microscaled 4-bit matrices x [rows, cin], w [cout, cin]; y [rows, cout] of type dt."""
-    _check(lib().alcs_mx4_product(_addr(x), _addr(x_scales), rows, _addr(w), _addr(w_scales), cout, cin, _addr(y), _addr(bias),
-                                  _addr(residual), flags, dt, _stream(stream)), "alcs_mx4_product")
+    st = _native().mx4_product(x, x_scales, rows, w, w_scales, cout, cin, y, bias, residual, flags, dt, stream)
+    if st is None:
+        st = lib().alcs_mx4_product(_addr(x), _addr(x_scales), rows, _addr(w), _addr(w_scales), cout, cin, _addr(y), _addr(bias),
+                                    _addr(residual), flags, dt, _stream(stream))
+    if st != ALCS_OK:
+        _check(st, "alcs_mx4_product")
 
 
 def alcs_mx4_status() -> int:
