@@ -471,10 +471,11 @@ ALCS_API int alcs_spconv2d_plan(const alcs_packed* w, int n, int cin, int h, int
  * pass needs it where a group's part of an image is spread over more thread blocks than can exchange sums directly; NULL and 0 where
  * that function says 0).  Its content matters only within a call; calls that may overlap on the GPU need one each, and so do
  * captured graphs that may.
- * All buffers belong to the current device.  One to four kernels on cuda_stream; no allocation, no synchronisation.  n == 0 or
+ * All buffers belong to the current device.  One to three kernels on cuda_stream; no allocation, no synchronisation.  n == 0 or
  * h*wd == 0 is a successful no-op, but for dgamma and dbeta, which become 0.
  * Errors: INVALID_ARG (null, misaligned or overlapping buffers, host memory, negative sizes, groups < 1, an eps that is negative or not finite, both
  * activations, workspace too small), SHAPE (c not a multiple of groups, h*wd or n*c of 2^30 and more, c above 65536),
+ * UNSUPPORTED (more than 8192 channels per group),
  * STATE (memory of another device), CUDA.
  * ------------------------------------------------------------------------------------------- */
 ALCS_API size_t alcs_group_norm_workspace(int n, int h, int wd, int c, int groups, alcs_dtype dt);
@@ -523,10 +524,11 @@ ALCS_API int alcs_mx4_dequantize(const void* data, const void* scales, int rows,
 ALCS_API int alcs_mx4_product(const void* x, const void* x_scales, int rows, const void* w, const void* w_scales, int cout, int cin,
                               void* y, const float* bias, const void* residual, unsigned flags, alcs_dtype dt, void* cuda_stream);
 /*
- * alcs_mx4_status: the error word of the current device's alcs_mx4_product calls (synchronises with the device).  *code is 0 unless a
- * kernel gave up one of its bounded waits: 1 = for data, 2 = for a free pipeline stage; the outputs of that launch are then incomplete.
+ * alcs_dense_status: the error word of the current device's alcs_group_norm, alcs_group_norm_backward and alcs_mx4_product calls
+ * (synchronises with the device).  *code is 0 unless a kernel gave up one of its bounded waits: 1 = for data, 2 = for a free pipeline stage; the
+ * outputs of that launch are then incomplete.
  */
-ALCS_API int alcs_mx4_status(int* code);
+ALCS_API int alcs_dense_status(int* code);
 
 /* ---------------------------------------------------------------------------------------------
  * Latency model and projection with bisection.

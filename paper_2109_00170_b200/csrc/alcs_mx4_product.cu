@@ -34,7 +34,7 @@ constexpr int kMaxSplit = 8;
 constexpr int kScaleBytes = 512;
 static_assert(kAccCols + 12 * kMaxStages <= 512, "tensor memory");
 
-__device__ int g_error;      // see alcs_mx4_status
+__device__ int g_error;      // see alcs_dense_status
 
 struct Operand {
     const unsigned char *data, *scales;
@@ -442,7 +442,7 @@ ALCS_API int alcs_mx4_product(const void* x, const void* x_scales, int rows, con
                                                                                      : launch<__nv_bfloat16>(a, blocks, smem, dev, st);
 }
 
-ALCS_API int alcs_mx4_status(int* code)
+ALCS_API int alcs_dense_status(int* code)
 {
     using namespace alcs;
     if (!code) return ALCS_ERR_INVALID_ARG;

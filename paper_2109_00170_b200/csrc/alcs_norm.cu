@@ -4,41 +4,52 @@
 //     dz = dy act'(z), t = gamma dz:  dbeta = sum dz, dgamma = sum dz xh, dx = rstd (t - mean t - xh mean(t xh))
 //
 // Bound by memory: x has to be read and y written once (backward: x, dy and dx), and a group's statistics need all of its values before
-// the first output.  So a group's part of an image is kept on chip between the two: a work item is a span of neighbouring groups
-// (their channels are 64 to 128 bytes of a pixel where that is possible: whole sectors of memory) of one image, its pixels are
-// shared out to the blocks of a cluster, and a block holds its share in registers, 16 bytes per load and up to 16 loads per thread in flight.
-// A thread keeps to its channels, whose parameters stay in registers.  The sums go through shared memory, in a fixed order, and
-// between the cluster's blocks through distributed shared memory.
-// Where a span's pixels do not fit a cluster, three passes: statistics of chunks of pixels, their union, and the outputs from a second reading of x.
+// the first output.
 //
-// The variance is that of values with a mean taken off: every block subtracts the mean of its own share, and shares are united by
-// M2 = sum M2_k + sum n_k (mean_k - mean)^2, which has no cancellation where the mean is large.  All of it in fp32.
+// One pass: a group's part of an image is kept on chip between the two.  A work item is a span of neighbouring groups (their channels are 64 to 128 bytes
+// of a pixel where that is possible: whole sectors of memory) of one image; its pixels are shared out to the blocks of a cluster, and a block holds its
+// share in shared memory, which cp.async fills without holding registers.  A thread keeps to its channels.  Sums go through shared memory, in a fixed
+// order, and between the cluster's blocks through distributed shared memory.  What it costs over a copy is the sums: all blocks of an SM tend to be at them
+// at the same time, with memory idle (64 images of 56x56x128, bf16: 33 us; a copy of them 18; without the sums 20; floor 15.7 at 6.5 TB/s).
+//
+// Two passes: sums of chunks of pixels, then the outputs from a second reading, which L2 serves as far as it holds x (and dy).  For spans that do
+// not fit a cluster, and for large calls of the backward pass.  Every thread keeps 8 loads (4 of x and dy each) on their way to slots of its own in
+// shared memory: with as many registers instead, a third of the bytes were in flight (backward of 64 images of 56x56x256, SiLU: 143 us, then 105:
+// 46 and 51 us for the passes).
+//
+// The variance is that of values with a mean taken off: a thread's run of at most 32 loads (one pass: what it holds) is summed less its first value, runs are
+// united by M2 = M2_a + M2_b + n_a n_b / n (mean_a - mean_b)^2, which has no cancellation where the mean is large.  All of it in fp32.
 #include <algorithm>
-#include <atomic>
 #include <cmath>
+#include <mutex>
+#include <set>
 
 #include "alcs_dense.h"
+#include "alcs_tc.h"
 
 namespace alcs {
 namespace {
 
-constexpr int kSplitThreads = 256;
-constexpr int kMaxThreads = 512;
+constexpr int kThreads = 128, kSplitThreads = 256;      // one pass; two passes
+constexpr int kMaxCluster = 16;
+constexpr int kMaxGroupChannels = 8192;     // (their sums stand in shared memory)
 constexpr int kMaxSpanGroups = 64;          // groups of a span
-constexpr int kBatch = 8;                   // loads in flight of the three-pass kernels
-enum { kNone = 0, kRelu = 1, kSilu = 2 };
 
 struct Args {
     const void *x, *dy;
     void* out;                   // y, dx
     const float *gamma, *beta;
     float *mean, *rstd;          // stored by the forward, read by the backward pass
-    float *part, *sums, *means;  // workspace: see Workspace
+    float *part, *sums;          // workspace: see Workspace
     int n, hw, c, groups, cg;    // cg: channels per group
     int gs, spans;               // groups per span
     int chunk, chunks;           // pixels per block, blocks per (span, image)
+    int loads;                   // one pass: loads per thread
+    int span_ch;                 // channels per span, rounded up to a multiple of 4
+    int whole;                   // a load's channels lie in one group
+    TcDiv cdiv, vdiv;            // by cg; by the loads of a group
     float eps;
-    int act;
+    int relu, silu;
 };
 
 // E neighbouring elements as they lie in memory.
@@ -76,34 +87,167 @@ __device__ __forceinline__ void store(T* p, const float (&v)[E])
     else *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()));
 }
 
-__device__ __forceinline__ float activate(float z, int act)
-{
-    if (act == kRelu) return fmaxf(z, 0.0f);
-    if (act == kSilu) return __fdividef(z, 1.0f + __expf(-z));      // (a few units in the last place of fp32)
-    return z;
-}
-// dy * act'(z)
-__device__ __forceinline__ float activate_back(float z, float dy, int act)
-{
-    if (act == kRelu) return z > 0.0f ? dy : 0.0f;
-    if (act == kSilu) {
-        const float s = __fdividef(1.0f, 1.0f + __expf(-z));
-        return dy * (s * fmaf(z, 1.0f - s, 1.0f));
+// d = a + b, a - b, a * b, a * b + c on E elements, two per instruction.
+#define ALCS_PAIRS(name, op)                                                                                                                            \
+    template <int E>                                                                                                                                    \
+    __device__ __forceinline__ void name(float (&d)[E], const float (&a)[E], const float (&b)[E])                                                       \
+    {                                                                                                                                                   \
+        if constexpr (E == 1) asm(op ".f32 %0, %1, %2;" : "=f"(d[0]) : "f"(a[0]), "f"(b[0]));                                                           \
+        else                                                                                                                                            \
+            _Pragma("unroll") for (int i = 0; i < E; i += 2)                                                                                            \
+                asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t" op ".f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"            \
+                    : "=f"(d[i]), "=f"(d[i + 1]) : "f"(a[i]), "f"(a[i + 1]), "f"(b[i]), "f"(b[i + 1]));                                                 \
     }
-    return dy;
+ALCS_PAIRS(add, "add.rn")
+ALCS_PAIRS(sub, "sub.rn")
+ALCS_PAIRS(mul, "mul.rn")
+template <int E>
+__device__ __forceinline__ void fma(float (&d)[E], const float (&a)[E], const float (&b)[E], const float (&c)[E])
+{
+    if constexpr (E == 1) d[0] = fmaf(a[0], b[0], c[0]);
+    else
+#pragma unroll
+        for (int i = 0; i < E; i += 2)
+            asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+                : "=f"(d[i]), "=f"(d[i + 1]) : "f"(a[i]), "f"(a[i + 1]), "f"(b[i]), "f"(b[i + 1]), "f"(c[i]), "f"(c[i + 1]));
+}
+template <int E>
+__device__ __forceinline__ void set(float (&d)[E], float v)
+{
+#pragma unroll
+    for (int j = 0; j < E; ++j) d[j] = v;
+}
+// E floats of shared memory, 4 E bytes aligned to their size up to 16
+template <int E>
+__device__ __forceinline__ void load_shared(float (&d)[E], const float* p)
+{
+    if constexpr (E == 1) d[0] = p[0];
+    else
+#pragma unroll
+        for (int j = 0; j < E; j += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(p + j);
+            d[j] = f.x; d[j + 1] = f.y; d[j + 2] = f.z; d[j + 3] = f.w;
+        }
+}
+template <int E>
+__device__ __forceinline__ void store_shared(float* p, const float (&d)[E])
+{
+    if constexpr (E == 1) p[0] = d[0];
+    else
+#pragma unroll
+        for (int j = 0; j < E; j += 4) *reinterpret_cast<float4*>(p + j) = make_float4(d[j], d[j + 1], d[j + 2], d[j + 3]);
+}
+
+// s = 1 / (1 + exp(-z)).  What bounds SiLU is the special function unit: two neighbours share a reciprocal (r = 1 / (a b), 1 / a = r b), so that an
+// element takes it one and a half times.  exp(-z) stays below 2^62 for that, so s is not below 2^-62.  Each instruction is good to 2^-22 or so.
+template <int E>
+__device__ __forceinline__ void sigmoid(float (&s)[E], const float (&z)[E])
+{
+    float k[E], one[E];
+    set<E>(k, -1.4426950408889634f);
+    set<E>(one, 1.0f);
+    mul<E>(s, z, k);
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        s[j] = fminf(s[j], 62.0f);      // (NaN, too, which its own z brings back, so that a neighbour's stays its own)
+        asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(s[j]));
+    }
+    add<E>(s, s, one);
+    if constexpr (E == 1) {
+        asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(s[0]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < E; j += 2) {
+            float r = s[j] * s[j + 1];
+            asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(r));
+            const float first = r * s[j + 1];
+            s[j + 1] = r * s[j];
+            s[j] = first;
+        }
+    }
+}
+
+template <bool SILU, int E>
+__device__ __forceinline__ void activate(float (&z)[E], bool relu)
+{
+    if (SILU) {
+        float s[E];
+        sigmoid<E>(s, z);
+        mul<E>(z, z, s);
+    } else if (relu) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) z[j] = fmaxf(z[j], 0.0f);
+    }
+}
+// d = dy * act'(z)
+template <bool SILU, int E>
+__device__ __forceinline__ void activate_back(float (&d)[E], float (&z)[E], bool relu)
+{
+    if (SILU) {      // s (1 + z (1 - s)) = s + (z s) (1 - s)
+        float s[E], one[E];
+        set<E>(one, 1.0f);
+        sigmoid<E>(s, z);
+        mul<E>(z, z, s);
+        sub<E>(one, one, s);
+        fma<E>(s, z, one, s);
+        mul<E>(d, d, s);
+    } else if (relu) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) d[j] = z[j] > 0.0f ? d[j] : 0.0f;
+    }
 }
 
 __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float ld_rank(const float* p, int rank)      // the same place in another block's shared memory
+__device__ __forceinline__ float2 ld_rank(const float2* p, int rank)      // the same place in another block's shared memory
 {
     unsigned at;
-    float v;
+    float2 v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((unsigned)__cvta_generic_to_shared(p)), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
     return v;
+}
+// Sum over the neighbouring `n` lanes (a power of two)
+__device__ __forceinline__ float lanes_sum(float v, int n)
+{
+    for (int o = n >> 1; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// E floats in two places of E elements of T (fp32: in the first alone)
+template <typename T, int E>
+__device__ __forceinline__ void put_dz(raw_t<T, E>* a, raw_t<T, E>* b, const float (&d)[E])
+{
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (E == 1) *a = __float_as_uint(d[0]);
+        else *a = Pack<float>::put(d);
+    } else if constexpr (E == 8) {
+        *a = Pack<float>::put(d);
+        *b = Pack<float>::put(d + 4);
+    } else if constexpr (E == 4) {
+        *a = make_uint2(__float_as_uint(d[0]), __float_as_uint(d[1]));
+        *b = make_uint2(__float_as_uint(d[2]), __float_as_uint(d[3]));
+    } else {
+        *a = (unsigned short)(__float_as_uint(d[0]) & 0xffffu);
+        *b = (unsigned short)(__float_as_uint(d[0]) >> 16);
+    }
+}
+template <typename T, int E>
+__device__ __forceinline__ void get_dz(const raw_t<T, E>* a, const raw_t<T, E>* b, float (&d)[E])
+{
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (E == 1) d[0] = __uint_as_float(*a);
+        else Pack<float>::get(*a, d);
+    } else if constexpr (E == 8) {
+        Pack<float>::get(*a, d);
+        Pack<float>::get(*b, d + 4);
+    } else if constexpr (E == 4) {
+        const uint2 x = *a, y = *b;
+        d[0] = __uint_as_float(x.x); d[1] = __uint_as_float(x.y); d[2] = __uint_as_float(y.x); d[3] = __uint_as_float(y.y);
+    } else {
+        d[0] = __uint_as_float((unsigned)*a | (unsigned)*b << 16);
+    }
 }
 __device__ __forceinline__ float warp_sum(float v)
 {
@@ -113,13 +257,14 @@ __device__ __forceinline__ float warp_sum(float v)
 }
 
 // Where a thread stands: its channels and pixels.
-template <int E>
+template <int E, int N>
 struct Place {
     int img, span, rank;
     int ch0, ng, nch, nv;        // span: first channel, groups, channels, vectors of E channels
     int rows, v, r;              // pixels side by side in the block; the thread's vector, pixel
     bool active;
     int p0, p1;                  // the block's pixels
+    Place() = default;
     __device__ __forceinline__ explicit Place(const Args& a)
     {
         const int unit = blockIdx.x / a.chunks;
@@ -130,8 +275,8 @@ struct Place {
         ng = min(a.gs, a.groups - span * a.gs);
         nch = ng * a.cg;
         nv = nch / E;
-        rows = max(1, (int)blockDim.x / nv);
-        r = nv <= (int)blockDim.x ? threadIdx.x / nv : 0;
+        rows = max(1, N / nv);
+        r = nv <= N ? threadIdx.x / nv : 0;
         v = threadIdx.x - r * nv;
         active = r < rows && v < nv;
         p0 = min(a.hw, rank * a.chunk);
@@ -139,51 +284,118 @@ struct Place {
     }
 };
 
-// Sums over the block's threads of values that belong to a thread's E channels, per group of the span: out[group].  `red`: E floats per thread.
-// WIDE spans (more vectors than threads) have one group.
-template <int E>
-__device__ __forceinline__ void sum_groups(const Place<E>& at, int cg, float (&acc)[E], float* red, float* out)
+// n / d of small numbers, d = a.cg
+__device__ __forceinline__ int over(int n, const TcDiv& d) { return (int)((unsigned long long)(unsigned)n * d.mul >> d.shift); }
+
+// Threads that share a group's values in the sums below: neighbouring lanes, as many as there are threads for.
+template <int N>
+__device__ __forceinline__ int lanes_of(int groups)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const bool whole = cg % E == 0;                          // a vector lies in one group
-    const int nv = min(at.nv, (int)blockDim.x);
-    const bool lanes = nv < 32 && (nv & (nv - 1)) == 0;       // lanes nv apart have the same vector
-    if (whole)
+    int l = 32;
+    while (l > 1 && l * groups > N) l >>= 1;
+    return l;
+}
+
+// n values of mean m and sum of squared distances q, united with as many again as `other` says
+struct Union {
+    float to, both;      // share of the other's; n times it
+    __device__ __forceinline__ Union(float n, float other) : to(n + other > 0.0f ? other / (n + other) : 0.0f), both(n * to) {}
+    __device__ __forceinline__ void operator()(float& m, float& q, float om, float oq) const
+    {
+        const float d = om - m;
+        m = fmaf(d, to, m);
+        q += fmaf(d * d, both, oq);
+    }
+};
+
+// Mean and sum of squared distances from it of the block's values of every group of the span: out[group].  A thread has n values of mean m and
+// squared distances q per channel.  `red`: 2 E floats per thread, `count`: one per thread.
+template <int N, int E>
+__device__ __forceinline__ void unite(const Place<E, N>& at, const Args& a, int n, float (&m)[E], float (&q)[E], float* red, float* count, float2* out)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const bool lanes = at.nv < 32 && (at.nv & (at.nv - 1)) == 0;       // lanes nv apart have the same vector
+    float k = (float)n;
+    if (a.whole && E > 1) {      // the thread's channels are one group's
+        float s = 0.0f, t = 0.0f;
 #pragma unroll
-        for (int j = 1; j < E; ++j) acc[0] += acc[j];
+        for (int j = 0; j < E; ++j) s += m[j];
+        s *= 1.0f / E;
+#pragma unroll
+        for (int j = 0; j < E; ++j) t += fmaf((m[j] - s) * k, m[j] - s, q[j]);
+        m[0] = s;
+        q[0] = t;
+        k *= E;
+    }
     if (lanes)
-        for (int o = nv; o < 32; o <<= 1)
+        for (int o = at.nv; o < 32; o <<= 1) {
+            const float other = __shfl_xor_sync(0xffffffffu, k, o);
+            const Union u(k, other);
 #pragma unroll
             for (int j = 0; j < E; ++j)
-                if (j == 0 || !whole) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], o);
-    const int per = whole ? nv : nv * E;                      // values of a row of `red`
-    const int rows = lanes ? warps : at.nv > nv ? 1 : at.rows;
-    if (lanes ? lane < nv : at.active) {
-        const int row = lanes ? warp : at.r, v = lanes ? lane : at.v;
-        if (whole) red[row * per + v] = acc[0];
-        else
-#pragma unroll
-            for (int j = 0; j < E; ++j) red[row * per + v * E + j] = acc[j];
-    }
-    __syncthreads();
-    const int m = at.nv > nv ? per : whole ? cg / E : cg;      // values of a group in a row
-    for (int g = warp; g < at.ng; g += warps) {
-        float s = 0.0f;
-        for (int e = lane; e < rows * m; e += 32) {
-            const int row = e / m;
-            s += red[row * per + g * m + e - row * m];
+                if (j == 0 || !a.whole) u(m[j], q[j], __shfl_xor_sync(0xffffffffu, m[j], o), __shfl_xor_sync(0xffffffffu, q[j], o));
+            k += other;
         }
-        s = warp_sum(s);
-        if (lane == 0) out[g] = s;
+    const int per = a.whole ? at.nv : at.nch, rows = lanes ? N / 32 : at.rows;
+    const int row = lanes ? warp : at.r, v = lanes ? lane : at.v;
+    if (lanes ? lane < at.nv : at.active) {
+        if (v == 0) count[row] = k;
+        float* const to = red + row * per;
+        if (a.whole) {
+            to[v] = m[0];
+            to[rows * per + v] = q[0];
+        } else {
+            store_shared<E>(to + v * E, m);
+            store_shared<E>(to + rows * per + v * E, q);
+        }
     }
     __syncthreads();
+    const int w = a.whole ? a.cg / E : a.cg;      // entries of a group in a row
+    const float inv = at.p1 > at.p0 ? 1.0f / ((float)(at.p1 - at.p0) * a.cg) : 0.0f;
+    const int l = lanes_of<N>(at.ng), sub = threadIdx.x & (l - 1);
+    for (int g0 = threadIdx.x / l; g0 - (int)threadIdx.x / l < at.ng; g0 += N / l) {      // (all threads: their lanes exchange sums)
+        const int g = min(g0, at.ng - 1);
+        const float* const from = red + g * w;
+        float s = 0.0f, t = 0.0f;
+        for (int e = sub; e < rows * w; e += l) {
+            const int r = over(e, a.whole ? a.vdiv : a.cdiv);
+            s = fmaf(from[r * per + e - r * w], count[r], s);
+        }
+        s = lanes_sum(s, l) * inv;
+        for (int e = sub; e < rows * w; e += l) {
+            const int r = over(e, a.whole ? a.vdiv : a.cdiv), i = r * per + e - r * w;
+            const float d = from[i] - s;
+            t += count[r] > 0.0f ? fmaf(d * d, count[r], from[rows * per + i]) : 0.0f;
+        }
+        t = lanes_sum(t, l);
+        if (sub == 0 && g == g0) out[g] = make_float2(s, t);
+    }
+}
+
+// gamma-weighted sums of the groups from the sums per channel: out[group].
+template <int N, int E>
+__device__ __forceinline__ void weigh(const Place<E, N>& at, const Args& a, const float* gamma, const float* rstd, const float* sums, float2* out)
+{
+    const int l = lanes_of<N>(at.ng), sub = threadIdx.x & (l - 1);
+    for (int g0 = threadIdx.x / l; g0 - (int)threadIdx.x / l < at.ng; g0 += N / l) {
+        const int g = min(g0, at.ng - 1);
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int j = sub; j < a.cg; j += l) {
+            const int c = g * a.cg + j;
+            s1 = fmaf(gamma[c], sums[c], s1);
+            s2 = fmaf(gamma[c], sums[at.nch + c], s2);
+        }
+        s1 = lanes_sum(s1, l);
+        s2 = lanes_sum(s2, l);
+        if (sub == 0 && g == g0) out[g] = make_float2(s1, s2 * rstd[g * a.cg]);
+    }
 }
 
 // Sums over the block's pixels of two values per channel: out[0 .. nch) and out[nch .. 2 nch).  `red`: 2 E floats per thread.
-template <int E>
-__device__ __forceinline__ void sum_channels(const Place<E>& at, float (&u)[E], float (&w)[E], float* red, float* out)
+template <int N, int E>
+__device__ __forceinline__ void sum_channels(const Place<E, N>& at, float (&u)[E], float (&w)[E], float* red, float* out)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, nv = at.nv;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = N / 32, nv = at.nv;
     const bool lanes = nv < 32 && (nv & (nv - 1)) == 0;
     if (lanes)
         for (int o = nv; o < 32; o <<= 1)
@@ -195,336 +407,391 @@ __device__ __forceinline__ void sum_channels(const Place<E>& at, float (&u)[E], 
     const int rows = lanes ? warps : at.rows;
     if (lanes ? lane < nv : at.active) {
         float* to = red + ((lanes ? warp : at.r) * nv + (lanes ? lane : at.v)) * E;
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            to[j] = u[j];
-            to[rows * at.nch + j] = w[j];
-        }
+        store_shared<E>(to, u);
+        store_shared<E>(to + rows * at.nch, w);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * at.nch; i += blockDim.x) {
-        const int k = i >= at.nch, ch = i - k * at.nch;
+    for (int i = threadIdx.x; i < 2 * at.nch; i += N) {
+        const float* from = red + (i >= at.nch ? (rows - 1) * at.nch : 0) + i;
         float s = 0.0f;
-        for (int row = 0; row < rows; ++row) s += red[(k * rows + row) * at.nch + ch];
+#pragma unroll 4
+        for (int row = 0; row < rows; ++row) s += from[row * at.nch];
         out[i] = s;
     }
     __syncthreads();
 }
 
-// gamma, beta, mean and rstd of a thread's channels.
-template <int E>
-struct Channels {
-    float gamma[E], beta[E], mean[E], rstd[E];
-    __device__ __forceinline__ void params(const Args& a, int ch)
-    {
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            gamma[j] = a.gamma ? __ldg(a.gamma + ch + j) : 1.0f;
-            beta[j] = a.beta ? __ldg(a.beta + ch + j) : 0.0f;
-        }
-    }
-    // from arrays of groups, the first of which is that of channel 0 of `ch`
-    __device__ __forceinline__ void stats(const float* m, const float* s, int ch, int cg)
-    {
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const int g = (ch + j) / cg;
-            mean[j] = m[g];
-            rstd[j] = s[g];
-        }
-    }
-};
-
-template <typename T, int E>
-__device__ __forceinline__ void normalise(const raw_t<T, E>& raw, T* to, const Channels<E>& ch, int act)
-{
-    float v[E];
-    get<T, E>(raw, v);
-#pragma unroll
-    for (int j = 0; j < E; ++j) v[j] = activate(fmaf((v[j] - ch.mean[j]) * ch.rstd[j], ch.gamma[j], ch.beta[j]), act);
-    store<T, E>(to, v);
-}
-
 // ---------------------------------------------------------------------------------------------
-// One pass: a block holds its pixels of a span in registers, V loads per thread.
+// One pass: a block holds its pixels of a span in shared memory, slot [i][thread] the thread's i-th load.  A thread reads only what it has
+// fetched itself, so that no barrier stands between.
 
-template <typename T, int E, int V>
-__global__ void __launch_bounds__(kMaxThreads, V <= 4 ? 2 : 1) norm_kernel(const Args a)
+template <int B>
+__device__ __forceinline__ void fetch_async(void* to, const void* from)
 {
-    extern __shared__ __align__(16) float red[];
-    __shared__ float own_mean[kMaxSpanGroups], own_m2[kMaxSpanGroups], mean[kMaxSpanGroups], rstd[kMaxSpanGroups];
-    const Place<E> at(a);
+    const unsigned at = (unsigned)__cvta_generic_to_shared(to);
+    if constexpr (B == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(B) : "memory");
+}
+// The thread's n loads, `step` elements apart, on their way to its slots.
+template <typename T, int E>
+__device__ __forceinline__ void fetch(raw_t<T, E>* slot, const T* x, size_t step, int n)
+{
+#pragma unroll 4
+    for (int i = 0; i < n; ++i, x += step) {
+        if constexpr (E * sizeof(T) >= 4) fetch_async<E * (int)sizeof(T)>(slot + i * kThreads, x);
+        else slot[i * kThreads] = load<T, E>(x);
+    }
+}
+__device__ __forceinline__ void fetched() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+__device__ __forceinline__ int pixels_of(const Args& a, int k) { return max(0, min(a.hw, (k + 1) * a.chunk) - k * a.chunk); }      // of block k of a cluster
+
+template <typename T, int E, bool SILU>
+__global__ void __launch_bounds__(kThreads, 8) norm_kernel(const Args a)
+{
+    extern __shared__ __align__(16) float red[];      // 2 E floats per thread; per channel; slots
+    __shared__ float count[kThreads];
+    __shared__ float2 own[kMaxSpanGroups];             // of the block's pixels: mean, squared distances from it
+    const Place<E, kThreads> at(a);
+    float* const mean = red + 2 * E * kThreads;        // of the image, per channel
+    float* const scale = mean + a.span_ch;             // rstd * gamma, beta
+    float* const shift = scale + a.span_ch;
+    raw_t<T, E>* const slot = reinterpret_cast<raw_t<T, E>*>(shift + a.span_ch) + threadIdx.x;
     const int ch = at.v * E;
     let_next_start();
     wait_for_previous();
-    Channels<E> par;
-    if (at.active) par.params(a, at.ch0 + ch);
     const size_t first = ((size_t)at.img * a.hw + at.p0 + at.r) * a.c + at.ch0 + ch, step = (size_t)at.rows * a.c;
-    const T* const x = static_cast<const T*>(a.x) + first;
-    const int mine = at.active ? at.p1 - at.p0 - at.r : 0;      // pixels from the thread's first on
-    raw_t<T, E> raw[V];
+    const int n = at.active ? max(0, at.p1 - at.p0 - at.r + at.rows - 1) / at.rows : 0;      // loads
+    fetch<T, E>(slot, static_cast<const T*>(a.x) + first, step, n);
+    for (int i = threadIdx.x; i < at.nch; i += kThreads) {
+        scale[i] = a.gamma ? __ldg(a.gamma + at.ch0 + i) : 1.0f;
+        shift[i] = a.beta ? __ldg(a.beta + at.ch0 + i) : 0.0f;
+    }
+    fetched();
+    // Sums of the thread's values, and of their squares, less the first one: of n values the square of the mean is then at most n times the
+    // sum of squared distances, and n is small.
+    float k[E], s[E], q[E];
+    set<E>(s, 0.0f);
+    set<E>(q, 0.0f);
+    if (n) get<T, E>(slot[0], k);
+#pragma unroll 4
+    for (int i = 1; i < n; ++i) {
+        float v[E];
+        get<T, E>(slot[i * kThreads], v);
+        sub<E>(v, v, k);
+        add<E>(s, s, v);
+        fma<E>(q, v, v, q);
+    }
+    const float inv = n ? 1.0f / (float)n : 0.0f;
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (i * at.rows < mine) raw[i] = load<T, E>(x + i * step);
-    float acc[E] = {};
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (i * at.rows < mine) {
-            float v[E];
-            get<T, E>(raw[i], v);
-#pragma unroll
-            for (int j = 0; j < E; ++j) acc[j] += v[j];
-        }
-    sum_groups<E>(at, a.cg, acc, red, own_mean);
-    const float own = (float)(at.p1 - at.p0) * a.cg, inv = own > 0.0f ? 1.0f / own : 0.0f;
-    if (threadIdx.x < at.ng) own_mean[threadIdx.x] *= inv;
-    __syncthreads();
-    if (at.active) par.stats(own_mean, own_mean, ch, a.cg);
-#pragma unroll
-    for (int j = 0; j < E; ++j) acc[j] = 0.0f;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (i * at.rows < mine) {
-            float v[E];
-            get<T, E>(raw[i], v);
-#pragma unroll
-            for (int j = 0; j < E; ++j) acc[j] = fmaf(v[j] - par.mean[j], v[j] - par.mean[j], acc[j]);
-        }
-    sum_groups<E>(at, a.cg, acc, red, own_m2);
+    for (int j = 0; j < E; ++j) {
+        const float d = s[j] * inv;
+        q[j] = fmaxf(fmaf(-d, s[j], q[j]), 0.0f * q[j]);      // (a NaN stays one)
+        s[j] = n ? k[j] + d : 0.0f;                           // the thread's mean
+    }
+    unite<kThreads, E>(at, a, n, s, q, red, count, own);
     if (a.chunks > 1) cluster_sync();
-    if (threadIdx.x < at.ng) {
-        const int g = threadIdx.x;
-        float m = 0.0f, m2 = 0.0f;
-        const float total = (float)a.hw * a.cg;
-        if (a.chunks == 1) {
-            m = own_mean[g];
-            m2 = own_m2[g];
-        } else {
-            float sum = 0.0f;
-#pragma unroll 1
-            for (int k = 0; k < a.chunks; ++k) {
-                const int px = max(0, min(a.hw, (k + 1) * a.chunk) - k * a.chunk);
-                sum = fmaf(ld_rank(own_mean + g, k), (float)px * a.cg, sum);
+    else __syncthreads();
+    // Every block unites the cluster's, a lane per (group, block), and spreads a group's result over its channels.
+    const float total = 1.0f / ((float)a.hw * a.cg);
+    const int lane = threadIdx.x & 31;
+    for (int i = threadIdx.x; i - lane < at.ng * a.chunks; i += kThreads) {
+        const int g = min(i / a.chunks, at.ng - 1), r = i & (a.chunks - 1);      // (chunks: a power of two, at most 16)
+        const float w = (float)pixels_of(a, r) * a.cg;
+        const float2 o = a.chunks > 1 ? ld_rank(own + g, r) : own[g];
+        const float mu = w > 0.0f ? lanes_sum(o.x * w, a.chunks) * total : lanes_sum(0.0f, a.chunks) * total;
+        const float d = o.x - mu;
+        const float m2 = lanes_sum(w > 0.0f ? fmaf(d * d, w, o.y) : 0.0f, a.chunks);
+        const float rs = 1.0f / sqrtf(fmaf(m2, total, a.eps));
+        if (i < at.ng * a.chunks) {
+            for (int j = r; j < a.cg; j += a.chunks) {
+                mean[g * a.cg + j] = mu;
+                scale[g * a.cg + j] *= rs;
             }
-            m = sum / total;
-#pragma unroll 1
-            for (int k = 0; k < a.chunks; ++k) {
-                const int px = max(0, min(a.hw, (k + 1) * a.chunk) - k * a.chunk);
-                const float d = ld_rank(own_mean + g, k) - m;
-                m2 += ld_rank(own_m2 + g, k);
-                if (px > 0) m2 = fmaf(d * d, (float)px * a.cg, m2);
+            if (at.rank == 0 && r == 0) {
+                const size_t to = (size_t)at.img * a.groups + at.span * a.gs + g;
+                if (a.mean) a.mean[to] = mu;
+                if (a.rstd) a.rstd[to] = rs;
             }
         }
-        const float s = 1.0f / sqrtf(m2 / total + a.eps);
-        mean[g] = m;
-        rstd[g] = s;
-        if (at.rank == 0 && a.mean) a.mean[(size_t)at.img * a.groups + at.span * a.gs + g] = m;
-        if (at.rank == 0 && a.rstd) a.rstd[(size_t)at.img * a.groups + at.span * a.gs + g] = s;
     }
     __syncthreads();
     if (a.chunks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // done with the others' shared memory
-    if (at.active) par.stats(mean, rstd, ch, a.cg);
-    T* const y = static_cast<T*>(a.out) + first;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (i * at.rows < mine) normalise<T, E>(raw[i], y + i * step, par, a.act);
+    if (n) {
+        T* y = static_cast<T*>(a.out) + first;
+        load_shared<E>(k, mean + ch);
+        load_shared<E>(s, scale + ch);
+        load_shared<E>(q, shift + ch);
+#pragma unroll 2
+        for (int i = 0; i < n; ++i, y += step) {
+            float v[E];
+            get<T, E>(slot[i * kThreads], v);
+            sub<E>(v, v, k);
+            fma<E>(v, v, s, q);
+            activate<SILU, E>(v, a.relu);
+            store<T, E>(y, v);
+        }
+    }
     __syncwarp();
     if (a.chunks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-template <typename T, int E, int V>
-__global__ void __launch_bounds__(kMaxThreads, V <= 2 ? 2 : 1) norm_back_kernel(const Args a)
+// With SiLU, dz of the first pass is kept for the second, in the place of dy (and, of 16 bits, in as much again): to compute it again would
+// take the special function unit longer than memory takes for the rest.
+template <typename T, int E, bool SILU>
+__global__ void __launch_bounds__(kThreads, 6) norm_back_kernel(const Args a)
 {
-    extern __shared__ __align__(16) float red[];      // 2 E floats per thread; sums per channel: the block's, the image's
-    __shared__ float k1[kMaxSpanGroups], k2[kMaxSpanGroups];
-    const Place<E> at(a);
-    const int ch = at.v * E, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float* const own = red + 2 * E * blockDim.x;
-    float* const all = own + 2 * at.nch;
+    extern __shared__ __align__(16) float red[];      // 2 E floats per thread; per channel; slots of x, of dy or dz
+    __shared__ float2 own[kMaxSpanGroups];             // the block's sums of gamma dz and gamma dz xh
+    const Place<E, kThreads> at(a);
+    float* const mean = red + 2 * E * kThreads;
+    float* const rstd = mean + a.span_ch;
+    float* const gamma = rstd + a.span_ch;
+    float* const beta = gamma + a.span_ch;
+    float* const sums = beta + a.span_ch;              // the block's, two per channel
+    raw_t<T, E>* const slot = reinterpret_cast<raw_t<T, E>*>(sums + 2 * a.span_ch) + threadIdx.x;
+    raw_t<T, E>* const dslot = slot + a.loads * kThreads;
+    // dz: E floats, the first half where dy is (16 bits)
+    raw_t<T, E>* const dslot2 = dslot + a.loads * kThreads;
+    const int ch = at.v * E, lane = threadIdx.x & 31;
     let_next_start();
     wait_for_previous();
     const size_t first = ((size_t)at.img * a.hw + at.p0 + at.r) * a.c + at.ch0 + ch, step = (size_t)at.rows * a.c;
-    const int mine = at.active ? at.p1 - at.p0 - at.r : 0;
-    const T* const x = static_cast<const T*>(a.x) + first;
-    const T* const dy = static_cast<const T*>(a.dy) + first;
-    raw_t<T, E> raw[V], draw[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (i * at.rows < mine) {
-            raw[i] = load<T, E>(x + i * step);
-            draw[i] = load<T, E>(dy + i * step);
-        }
-    Channels<E> par;
-    if (at.active) {
-        const size_t g0 = (size_t)at.img * a.groups + at.span * a.gs;
-        par.params(a, at.ch0 + ch);
-        par.stats(a.mean + g0, a.rstd + g0, ch, a.cg);
+    const int n = at.active ? max(0, at.p1 - at.p0 - at.r + at.rows - 1) / at.rows : 0;
+    fetch<T, E>(slot, static_cast<const T*>(a.x) + first, step, n);
+    fetch<T, E>(dslot, static_cast<const T*>(a.dy) + first, step, n);
+    for (int i = threadIdx.x; i < at.nch; i += kThreads) {
+        const size_t g = (size_t)at.img * a.groups + at.span * a.gs + over(i, a.cdiv);
+        mean[i] = a.mean[g];
+        rstd[i] = a.rstd[g];
+        gamma[i] = a.gamma ? __ldg(a.gamma + at.ch0 + i) : 1.0f;
+        beta[i] = a.beta ? __ldg(a.beta + at.ch0 + i) : 0.0f;
     }
-    float u[E] = {}, w[E] = {};
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (i * at.rows < mine) {
-            float v[E], d[E];
-            get<T, E>(raw[i], v);
-            get<T, E>(draw[i], d);
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const float xh = (v[j] - par.mean[j]) * par.rstd[j];
-                const float dz = activate_back(fmaf(xh, par.gamma[j], par.beta[j]), d[j], a.act);
-                u[j] += dz;
-                w[j] = fmaf(dz, xh, w[j]);
-            }
-        }
-    sum_channels<E>(at, u, w, red, own);
-    if (a.chunks > 1) cluster_sync();
-    for (int i = threadIdx.x; i < 2 * at.nch; i += blockDim.x) {
-        float s = 0.0f;
-        if (a.chunks == 1) s = own[i];
-        else
+    __syncthreads();
+    float m[E], g[E], b[E], u[E], w[E];
+    if (n) {
+        load_shared<E>(m, mean + ch);
+        load_shared<E>(g, gamma + ch);
+        load_shared<E>(u, rstd + ch);
+        load_shared<E>(b, beta + ch);
+        mul<E>(g, g, u);
+    }
+    set<E>(u, 0.0f);
+    set<E>(w, 0.0f);
+    fetched();
 #pragma unroll 1
-            for (int k = 0; k < a.chunks; ++k) s += ld_rank(own + i, k);
-        all[i] = s;
-        if (at.rank == 0 && a.sums) {
-            const int k = i >= at.nch, c = at.ch0 + i - k * at.nch;
-            a.sums[((size_t)at.img * 2 + k) * a.c + c] = s;
-        }
+    for (int i = 0; i < n; ++i) {
+        float v[E], d[E], z[E];
+        get<T, E>(slot[i * kThreads], v);
+        get<T, E>(dslot[i * kThreads], d);
+        sub<E>(v, v, m);
+        fma<E>(z, v, g, b);
+        activate_back<SILU, E>(d, z, a.relu);
+        add<E>(u, u, d);
+        fma<E>(w, d, v, w);      // (times rstd below)
+        if constexpr (SILU) put_dz<T, E>(dslot + i * kThreads, dslot2 + i * kThreads, d);
+    }
+    sum_channels<kThreads, E>(at, u, w, red, sums);
+    for (int i = threadIdx.x; i < at.nch; i += kThreads) {
+        float* const to = a.sums + ((size_t)at.img * a.chunks + at.rank) * 2 * a.c + at.ch0 + i;
+        to[0] = sums[i];
+        to[a.c] = sums[at.nch + i] * rstd[i];
+    }
+    weigh<kThreads, E>(at, a, gamma, rstd, sums, own);
+    if (a.chunks > 1) cluster_sync();
+    else __syncthreads();
+    const float inv = 1.0f / ((float)a.hw * a.cg);
+    for (int i = threadIdx.x; i - lane < at.ng * a.chunks; i += kThreads) {
+        const int q = min(i / a.chunks, at.ng - 1), k = i & (a.chunks - 1);
+        const float2 o = a.chunks > 1 ? ld_rank(own + q, k) : own[q];
+        const float r = rstd[q * a.cg];
+        const float s1 = lanes_sum(o.x, a.chunks) * inv * -r, s2 = lanes_sum(o.y, a.chunks) * inv * -r * r;
+        if (i < at.ng * a.chunks)
+            for (int j = k; j < a.cg; j += a.chunks) { red[q * a.cg + j] = s1; red[at.nch + q * a.cg + j] = s2; }
     }
     __syncthreads();
     if (a.chunks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    const float inv = 1.0f / ((float)a.hw * a.cg);
-    for (int g = warp; g < at.ng; g += blockDim.x >> 5) {
-        float s1 = 0.0f, s2 = 0.0f;
-        for (int j = lane; j < a.cg; j += 32) {
-            const int c = g * a.cg + j;
-            const float gm = a.gamma ? __ldg(a.gamma + at.ch0 + c) : 1.0f;
-            s1 = fmaf(gm, all[c], s1);
-            s2 = fmaf(gm, all[at.nch + c], s2);
-        }
-        s1 = warp_sum(s1);
-        s2 = warp_sum(s2);
-        if (lane == 0) { k1[g] = s1 * inv; k2[g] = s2 * inv; }
-    }
-    __syncthreads();
-    T* const dx = static_cast<T*>(a.out) + first;
-    if (at.active) {
-#pragma unroll
-        for (int j = 0; j < E; ++j) { u[j] = k1[(ch + j) / a.cg]; w[j] = k2[(ch + j) / a.cg]; }
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (i * at.rows < mine) {
+    if (n) {      // dx = (rstd gamma) dz - rstd k1 - (rstd^2 k2) (x - mean)
+        T* dx = static_cast<T*>(a.out) + first;
+        load_shared<E>(u, red + ch);
+        load_shared<E>(w, red + at.nch + ch);
+#pragma unroll 2
+        for (int i = 0; i < n; ++i, dx += step) {
             float v[E], d[E];
-            get<T, E>(raw[i], v);
-            get<T, E>(draw[i], d);
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const float xh = (v[j] - par.mean[j]) * par.rstd[j];
-                const float dz = activate_back(fmaf(xh, par.gamma[j], par.beta[j]), d[j], a.act);
-                v[j] = par.rstd[j] * (fmaf(par.gamma[j], dz, -u[j]) - xh * w[j]);
+            get<T, E>(slot[i * kThreads], v);
+            sub<E>(v, v, m);
+            if constexpr (SILU) {
+                get_dz<T, E>(dslot + i * kThreads, dslot2 + i * kThreads, d);
+            } else {
+                get<T, E>(dslot[i * kThreads], d);
+                if (a.relu) {
+                    float z[E];
+                    fma<E>(z, v, g, b);
+                    activate_back<false, E>(d, z, true);
+                }
             }
-            store<T, E>(dx + i * step, v);
+            fma<E>(v, v, w, u);
+            fma<E>(v, d, g, v);
+            store<T, E>(dx, v);
         }
+    }
     __syncwarp();
     if (a.chunks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // ---------------------------------------------------------------------------------------------
-// Three passes, for spans that do not fit.
+// Two passes: the sums of chunks of pixels, and the outputs from a second reading.  A block has a chunk of pixels and a span of as many groups as it
+// has threads for (a thread has all pixels of a column of loads, or every rows-th).
 
-// Mean and sum of squared distances from it of a chunk, per group: part[image][chunk][group][2].
-template <typename T, int E>
-__global__ void __launch_bounds__(kSplitThreads) stats_kernel(const Args a)
+// gamma, beta, mean and rstd of a thread's channels, of a span's first channel on
+template <int E>
+__device__ __forceinline__ void channels(const Args& a, int ch0, int ch, const float* mean, const float* rstd, float (&m)[E], float (&r)[E], float (&g)[E], float (&b)[E])
 {
-    extern __shared__ __align__(16) float red[];
-    __shared__ float mean[kMaxSpanGroups], m2[kMaxSpanGroups];
-    const Place<E> at(a);
+    int q = over(ch, a.cdiv), next = (q + 1) * a.cg - ch;      // the group, and the channels left in it
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        if (j == next) { ++q; next += a.cg; }
+        m[j] = mean[q];
+        r[j] = rstd[q];
+        g[j] = a.gamma ? __ldg(a.gamma + ch0 + ch + j) : 1.0f;
+        b[j] = a.beta ? __ldg(a.beta + ch0 + ch + j) : 0.0f;
+    }
+}
+
+constexpr int kRun = 32;       // loads whose squares are summed less the first one's (a multiple of kDeep)
+
+// A thread's column of n loads, D of them on their way to its slots of shared memory [D][thread]: for a kernel that keeps no more of what it reads, registers
+// would hold too few loads in flight.  Loops are unrolled D times, so that a slot's place is known.
+template <typename T, int E, int D>
+struct Column {
+    raw_t<T, E>* slot;
+    const T* next;
+    size_t step;
+    __device__ __forceinline__ Column(void* ring, const T* x, size_t step_) : slot(static_cast<raw_t<T, E>*>(ring) + threadIdx.x), next(x), step(step_) {}
+    __device__ __forceinline__ void ask(int j, bool any)      // the next load, for slot j
+    {
+        if (any) {
+            if constexpr (E * sizeof(T) >= 4) fetch_async<E * (int)sizeof(T)>(slot + j * kSplitThreads, next);
+            else slot[j * kSplitThreads] = load<T, E>(next);
+        }
+        next += step;
+    }
+    __device__ __forceinline__ const raw_t<T, E>& at(int j) const { return slot[j * kSplitThreads]; }
+};
+__device__ __forceinline__ void asked() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int D>
+__device__ __forceinline__ void wait_oldest() { asm volatile("cp.async.wait_group %0;" ::"n"(D - 1) : "memory"); }
+constexpr int kDeep = 8, kDeepBack = 4;      // of one tensor; of x and dy each
+
+// Mean and sum of squared distances from it of a chunk, per group: part[image][chunk][group][2].  A wide span is one group and one chunk's column
+// of loads after the other; its threads then unite theirs as if they were channels' of one load.
+template <typename T, int E>
+__global__ void __launch_bounds__(kSplitThreads, 4) stats_kernel(const Args a)
+{
+    extern __shared__ __align__(16) float red[];      // 2 E floats per thread; ring
+    __shared__ float count[kSplitThreads];
+    void* const ring = red + 2 * E * kSplitThreads;
+    const Place<E, kSplitThreads> at(a);
     let_next_start();
     wait_for_previous();
-    float m[E] = {}, q[E] = {}, count = 0.0f;      // of the thread's values, per channel (or, of a wide span, all of one group)
+    float s[E], q[E], n = 0.0f;
+    set<E>(s, 0.0f);
+    set<E>(q, 0.0f);
+    const bool wide = at.nv > kSplitThreads;
     for (int v = at.v; at.active && v < at.nv; v += kSplitThreads) {
-        const T* const x = static_cast<const T*>(a.x) + (size_t)at.img * a.hw * a.c + at.ch0 + v * E;
-        for (int p = at.p0 + at.r; p < at.p1; p += kBatch * at.rows) {
-            raw_t<T, E> raw[kBatch];
-            int k = 0;
+        const T* x = static_cast<const T*>(a.x) + ((size_t)at.img * a.hw + at.p0 + at.r) * a.c + at.ch0 + v * E;
+        const size_t step = (size_t)at.rows * a.c;
+        const int loads = (at.p1 - at.p0 - at.r + at.rows - 1) / at.rows;
+        Column<T, E, kDeep> col(ring, x, step);
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i)
-                if (p + i * at.rows < at.p1) { raw[i] = load<T, E>(x + (size_t)(p + i * at.rows) * a.c); ++k; }
-            float s[E] = {}, b[E] = {};
+        for (int j = 0; j < kDeep; ++j) { col.ask(j, j < loads); asked(); }
+        for (int i0 = 0; i0 < loads; i0 += kRun) {
+            float f[E], u[E], w[E];      // (as norm_kernel: less the first value, of a short run)
+            set<E>(u, 0.0f);
+            set<E>(w, 0.0f);
+            const int end = min(loads, i0 + kRun);
+            wait_oldest<kDeep>();
+            get<T, E>(col.at(0), f);
+            for (int i = i0; i < end; i += kDeep)
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i)
-                if (i < k) {
-                    float f[E];
-                    get<T, E>(raw[i], f);
-#pragma unroll
-                    for (int j = 0; j < E; ++j) s[j] += f[j];
-                }
-            const float kf = (float)k, inv = 1.0f / kf, total = count + kf;
-#pragma unroll
-            for (int j = 0; j < E; ++j) s[j] *= inv;
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i)
-                if (i < k) {
-                    float f[E];
-                    get<T, E>(raw[i], f);
-#pragma unroll
-                    for (int j = 0; j < E; ++j) b[j] = fmaf(f[j] - s[j], f[j] - s[j], b[j]);
-                }
-            const float share = kf / total, both = count * share;
+                for (int j = 0; j < kDeep; ++j)
+                    if (i + j < end) {
+                        wait_oldest<kDeep>();
+                        float d[E];
+                        get<T, E>(col.at(j), d);
+                        sub<E>(d, d, f);
+                        add<E>(u, u, d);
+                        fma<E>(w, d, d, w);
+                        col.ask(j, i + j + kDeep < loads);
+                        asked();
+                    }
+            const float run = (float)(end - i0), inv = 1.0f / run;
+            const Union both(n, run);
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                const float d = s[j] - m[j];
-                m[j] = fmaf(d, share, m[j]);
-                q[j] += fmaf(d * d, both, b[j]);
+                const float d = u[j] * inv;
+                w[j] = fmaxf(fmaf(-d, u[j], w[j]), 0.0f * w[j]);
+                both(s[j], q[j], f[j] + d, w[j]);
             }
-            count = total;
+            n += run;
         }
     }
-    float acc[E];
+    float2* const to = reinterpret_cast<float2*>(a.part) + ((size_t)at.img * a.chunks + at.rank) * a.groups + at.span * a.gs;
+    if (!wide) {
+        unite<kSplitThreads, E>(at, a, (int)n, s, q, red, count, to);
+        return;
+    }
+    // one group: all of the block's values
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float c = n;
 #pragma unroll
-    for (int j = 0; j < E; ++j) acc[j] = m[j] * count;
-    sum_groups<E>(at, a.cg, acc, red, mean);
-    const float inv = at.p1 > at.p0 ? 1.0f / ((float)(at.p1 - at.p0) * a.cg) : 0.0f;
-    if (threadIdx.x < at.ng) mean[threadIdx.x] *= inv;
+    for (int j = 1; j < E; ++j) {
+        const Union both(c, n);
+        both(s[0], q[0], s[j], q[j]);
+        c += n;
+    }
+    for (int o = 1; o < 32; o <<= 1) {
+        const float other = __shfl_xor_sync(0xffffffffu, c, o);
+        const Union both(c, other);
+        both(s[0], q[0], __shfl_xor_sync(0xffffffffu, s[0], o), __shfl_xor_sync(0xffffffffu, q[0], o));
+        c += other;
+    }
+    if (lane == 0) { red[warp] = s[0]; red[32 + warp] = q[0]; count[warp] = c; }
     __syncthreads();
-    if (at.active)
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const float d = m[j] - mean[at.nv > kSplitThreads ? 0 : (at.v * E + j) / a.cg];
-            acc[j] = fmaf(d * d, count, q[j]);
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < kSplitThreads / 32; ++i) {
+            const Union both(c, count[i]);
+            both(s[0], q[0], red[i], red[32 + i]);
+            c += count[i];
         }
-    else
-#pragma unroll
-        for (int j = 0; j < E; ++j) acc[j] = 0.0f;
-    sum_groups<E>(at, a.cg, acc, red, m2);
-    if (threadIdx.x < at.ng) {
-        float* to = a.part + (((size_t)at.img * a.chunks + at.rank) * a.groups + at.span * a.gs + threadIdx.x) * 2;
-        to[0] = mean[threadIdx.x];
-        to[1] = m2[threadIdx.x];
+        *to = make_float2(s[0], q[0]);
     }
 }
 
 // The union of the chunks' statistics, by every block for its groups, and the outputs.
-template <typename T, int E>
-__global__ void __launch_bounds__(kSplitThreads) apply_kernel(const Args a)
+template <typename T, int E, bool SILU>
+__global__ void __launch_bounds__(kSplitThreads, 4) apply_kernel(const Args a)
 {
+    extern __shared__ __align__(16) float ring[];
     __shared__ float mean[kMaxSpanGroups], rstd[kMaxSpanGroups];
-    const Place<E> at(a);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Place<E, kSplitThreads> at(a);
     let_next_start();
     wait_for_previous();
-    for (int g = warp; g < at.ng; g += kSplitThreads / 32) {
-        const float* const from = a.part + ((size_t)at.img * a.chunks * a.groups + at.span * a.gs + g) * 2;
-        const float total = (float)a.hw * a.cg;
+    const int l = lanes_of<kSplitThreads>(at.ng), sub_ = threadIdx.x & (l - 1);
+    const float total = (float)a.hw * a.cg;
+    for (int g0 = threadIdx.x / l; g0 - (int)threadIdx.x / l < at.ng; g0 += kSplitThreads / l) {
+        const int g = min(g0, at.ng - 1);
+        const float2* const from = reinterpret_cast<const float2*>(a.part) + (size_t)at.img * a.chunks * a.groups + at.span * a.gs + g;
         float s = 0.0f, m2 = 0.0f;
-        for (int k = lane; k < a.chunks; k += 32) s = fmaf(from[(size_t)k * a.groups * 2], (float)(min(a.hw, (k + 1) * a.chunk) - k * a.chunk) * a.cg, s);
-        const float m = warp_sum(s) / total;
-        for (int k = lane; k < a.chunks; k += 32) {
-            const float d = from[(size_t)k * a.groups * 2] - m;
-            m2 += fmaf(d * d, (float)(min(a.hw, (k + 1) * a.chunk) - k * a.chunk) * a.cg, from[(size_t)k * a.groups * 2 + 1]);
+        for (int k = sub_; k < a.chunks; k += l) s = fmaf(from[(size_t)k * a.groups].x, (float)pixels_of(a, k) * a.cg, s);
+        const float m = lanes_sum(s, l) / total;
+        for (int k = sub_; k < a.chunks; k += l) {
+            const float2 o = from[(size_t)k * a.groups];
+            m2 += fmaf((o.x - m) * (o.x - m), (float)pixels_of(a, k) * a.cg, o.y);
         }
-        m2 = warp_sum(m2);
-        const float r = 1.0f / sqrtf(m2 / total + a.eps);
-        if (lane == 0) {
+        m2 = lanes_sum(m2, l);
+        if (sub_ == 0 && g == g0) {
+            const float r = 1.0f / sqrtf(m2 / total + a.eps);
             mean[g] = m;
             rstd[g] = r;
             const size_t o = (size_t)at.img * a.groups + at.span * a.gs + g;
@@ -534,188 +801,200 @@ __global__ void __launch_bounds__(kSplitThreads) apply_kernel(const Args a)
     }
     __syncthreads();
     for (int v = at.v; at.active && v < at.nv; v += kSplitThreads) {
-        Channels<E> par;
-        par.params(a, at.ch0 + v * E);
-        par.stats(mean, rstd, v * E, a.cg);
-        const size_t first = (size_t)at.img * a.hw * a.c + at.ch0 + v * E;
-        const T* const x = static_cast<const T*>(a.x) + first;
-        T* const y = static_cast<T*>(a.out) + first;
-        for (int p = at.p0 + at.r; p < at.p1; p += kBatch * at.rows) {
-            raw_t<T, E> raw[kBatch];
+        float m[E], r[E], g[E], b[E];
+        channels<E>(a, at.ch0, v * E, mean, rstd, m, r, g, b);
+        mul<E>(r, r, g);
+        size_t first = ((size_t)at.img * a.hw + at.p0 + at.r) * a.c + at.ch0 + v * E;
+        const size_t step = (size_t)at.rows * a.c;
+        const T* x = static_cast<const T*>(a.x) + first;
+        T* y = static_cast<T*>(a.out) + first;
+        const int loads = (at.p1 - at.p0 - at.r + at.rows - 1) / at.rows;
+        Column<T, E, kDeep> col(ring, x, step);
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i)
-                if (p + i * at.rows < at.p1) raw[i] = load<T, E>(x + (size_t)(p + i * at.rows) * a.c);
+        for (int j = 0; j < kDeep; ++j) { col.ask(j, j < loads); asked(); }
+        for (int i = 0; i < loads; i += kDeep)
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i)
-                if (p + i * at.rows < at.p1) normalise<T, E>(raw[i], y + (size_t)(p + i * at.rows) * a.c, par, a.act);
-        }
+            for (int j = 0; j < kDeep; ++j)
+                if (i + j < loads) {
+                    wait_oldest<kDeep>();
+                    float f[E];
+                    get<T, E>(col.at(j), f);
+                    sub<E>(f, f, m);
+                    fma<E>(f, f, r, b);
+                    activate<SILU, E>(f, a.relu);
+                    store<T, E>(y, f);
+                    y += step;
+                    col.ask(j, i + j + kDeep < loads);
+                    asked();
+                }
     }
 }
 
-// sum dz and sum dz xh of a chunk, per channel: part[image][chunk][2][channel].
-template <typename T, int E>
-__global__ void __launch_bounds__(kSplitThreads) back_stats_kernel(const Args a)
+// sum dz and sum dz xh of a chunk, per channel: sums[image][chunk][2][channel]; times gamma, per group: part[image][chunk][group][2].
+template <typename T, int E, bool SILU>
+__global__ void __launch_bounds__(kSplitThreads, 3) back_stats_kernel(const Args a)
 {
-    extern __shared__ __align__(16) float red[];
-    const Place<E> at(a);
+    extern __shared__ __align__(16) float red[];      // 2 E floats per thread; rings; per channel: gamma, rstd, two sums
+    const Place<E, kSplitThreads> at(a);
+    void* const ring = red + 2 * E * kSplitThreads;
+    void* const dring = static_cast<raw_t<T, E>*>(ring) + kDeepBack * kSplitThreads;
+    float* const gamma = reinterpret_cast<float*>(static_cast<raw_t<T, E>*>(dring) + kDeepBack * kSplitThreads);
+    float* const rstd = gamma + a.span_ch;
+    float* const sums = rstd + a.span_ch;
     let_next_start();
     wait_for_previous();
-    const size_t g0 = (size_t)at.img * a.groups + at.span * a.gs;
-    float* const to = a.part + ((size_t)at.img * a.chunks + at.rank) * 2 * a.c + at.ch0;
-    float u[E] = {}, w[E] = {};
-    for (int v = at.v; at.active && v < at.nv; v += kSplitThreads) {
-        Channels<E> par;
-        par.params(a, at.ch0 + v * E);
-        par.stats(a.mean + g0, a.rstd + g0, v * E, a.cg);
-        const size_t first = (size_t)at.img * a.hw * a.c + at.ch0 + v * E;
-        const T* const x = static_cast<const T*>(a.x) + first;
-        const T* const dy = static_cast<const T*>(a.dy) + first;
-#pragma unroll
-        for (int j = 0; j < E; ++j) u[j] = w[j] = 0.0f;
-        for (int p = at.p0 + at.r; p < at.p1; p += kBatch / 2 * at.rows) {
-            raw_t<T, E> raw[kBatch / 2], draw[kBatch / 2];
-#pragma unroll
-            for (int i = 0; i < kBatch / 2; ++i)
-                if (p + i * at.rows < at.p1) {
-                    raw[i] = load<T, E>(x + (size_t)(p + i * at.rows) * a.c);
-                    draw[i] = load<T, E>(dy + (size_t)(p + i * at.rows) * a.c);
-                }
-#pragma unroll
-            for (int i = 0; i < kBatch / 2; ++i)
-                if (p + i * at.rows < at.p1) {
-                    float f[E], d[E];
-                    get<T, E>(raw[i], f);
-                    get<T, E>(draw[i], d);
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        const float xh = (f[j] - par.mean[j]) * par.rstd[j];
-                        const float dz = activate_back(fmaf(xh, par.gamma[j], par.beta[j]), d[j], a.act);
-                        u[j] += dz;
-                        w[j] = fmaf(dz, xh, w[j]);
-                    }
-                }
-        }
-        if (at.nv > kSplitThreads)      // a wide span: the thread has all of the chunk's pixels
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                to[v * E + j] = u[j];
-                to[a.c + v * E + j] = w[j];
-            }
+    const size_t q0 = (size_t)at.img * a.groups + at.span * a.gs;
+    for (int i = threadIdx.x; i < at.nch; i += kSplitThreads) {
+        gamma[i] = a.gamma ? __ldg(a.gamma + at.ch0 + i) : 1.0f;
+        rstd[i] = a.rstd[q0 + over(i, a.cdiv)];
     }
-    if (at.nv > kSplitThreads) return;
-    float* const sums = red + 2 * E * kSplitThreads;
-    sum_channels<E>(at, u, w, red, sums);
+    float u[E], w[E];
+    set<E>(u, 0.0f);
+    set<E>(w, 0.0f);
+    const bool wide = at.nv > kSplitThreads;
+    for (int v = at.v; at.active && v < at.nv; v += kSplitThreads) {
+        float m[E], g[E], b[E];
+        channels<E>(a, at.ch0, v * E, a.mean + q0, a.rstd + q0, m, u, g, b);
+        mul<E>(g, g, u);
+        set<E>(u, 0.0f);
+        set<E>(w, 0.0f);
+        const size_t first = ((size_t)at.img * a.hw + at.p0 + at.r) * a.c + at.ch0 + v * E, step = (size_t)at.rows * a.c;
+        const T* x = static_cast<const T*>(a.x) + first;
+        const T* dy = static_cast<const T*>(a.dy) + first;
+        const int loads = (at.p1 - at.p0 - at.r + at.rows - 1) / at.rows;
+        Column<T, E, kDeepBack> col(ring, x, step), dcol(dring, dy, step);
+#pragma unroll
+        for (int j = 0; j < kDeepBack; ++j) { col.ask(j, j < loads); dcol.ask(j, j < loads); asked(); }
+        for (int i = 0; i < loads; i += kDeepBack)
+#pragma unroll
+            for (int j = 0; j < kDeepBack; ++j)
+                if (i + j < loads) {
+                    wait_oldest<kDeepBack>();
+                    float f[E], d[E], z[E];
+                    get<T, E>(col.at(j), f);
+                    get<T, E>(dcol.at(j), d);
+                    sub<E>(f, f, m);
+                    if (SILU || a.relu) {
+                        fma<E>(z, f, g, b);
+                        activate_back<SILU, E>(d, z, a.relu);
+                    }
+                    add<E>(u, u, d);
+                    fma<E>(w, d, f, w);
+                    col.ask(j, i + j + kDeepBack < loads);
+                    dcol.ask(j, i + j + kDeepBack < loads);
+                    asked();
+                }
+        if (wide) {      // the thread has all of the chunk's pixels
+            store_shared<E>(sums + v * E, u);
+            store_shared<E>(sums + at.nch + v * E, w);
+        }
+    }
+    if (wide) __syncthreads();
+    else sum_channels<kSplitThreads, E>(at, u, w, red, sums);
+    float* const to = a.sums + ((size_t)at.img * a.chunks + at.rank) * 2 * a.c + at.ch0;
     for (int i = threadIdx.x; i < at.nch; i += kSplitThreads) {
         to[i] = sums[i];
-        to[a.c + i] = sums[at.nch + i];
+        to[a.c + i] = sums[at.nch + i] * rstd[i];
     }
+    weigh<kSplitThreads, E>(at, a, gamma, rstd, sums, reinterpret_cast<float2*>(a.part) + ((size_t)at.img * a.chunks + at.rank) * a.groups + at.span * a.gs);
 }
 
-// The chunks' sums of an image's group: sums[image][2][channel], means[image][group][2].  One block per (image, group).
-__global__ void __launch_bounds__(128) back_unite_kernel(const Args a)
+template <typename T, int E, bool SILU>
+__global__ void __launch_bounds__(kSplitThreads, 3) back_apply_kernel(const Args a)
 {
-    __shared__ float s1[4], s2[4];
+    extern __shared__ __align__(16) float ring[];
+    __shared__ float k1[kMaxSpanGroups], k2[kMaxSpanGroups];
+    void* const dring = reinterpret_cast<raw_t<T, E>*>(ring) + kDeepBack * kSplitThreads;
+    const Place<E, kSplitThreads> at(a);
     let_next_start();
     wait_for_previous();
-    const int img = blockIdx.x / a.groups, g = blockIdx.x - img * a.groups, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float t1 = 0.0f, t2 = 0.0f;
-    for (int j = threadIdx.x; j < a.cg; j += 128) {
-        const int c = g * a.cg + j;
-        const float* const from = a.part + (size_t)img * a.chunks * 2 * a.c + c;
-        float u = 0.0f, w = 0.0f;
-#pragma unroll 4
-        for (int k = 0; k < a.chunks; ++k) {
-            u += from[(size_t)k * 2 * a.c];
-            w += from[(size_t)k * 2 * a.c + a.c];
+    const size_t q0 = (size_t)at.img * a.groups + at.span * a.gs;
+    const int l = lanes_of<kSplitThreads>(at.ng), sub_ = threadIdx.x & (l - 1);
+    const float inv = 1.0f / ((float)a.hw * a.cg);
+    for (int g0 = threadIdx.x / l; g0 - (int)threadIdx.x / l < at.ng; g0 += kSplitThreads / l) {
+        const int g = min(g0, at.ng - 1);
+        const float2* const from = reinterpret_cast<const float2*>(a.part) + (size_t)at.img * a.chunks * a.groups + at.span * a.gs + g;
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int k = sub_; k < a.chunks; k += l) {
+            const float2 o = from[(size_t)k * a.groups];
+            s1 += o.x;
+            s2 += o.y;
         }
-        a.sums[(size_t)img * 2 * a.c + c] = u;
-        a.sums[((size_t)img * 2 + 1) * a.c + c] = w;
-        const float gm = a.gamma ? __ldg(a.gamma + c) : 1.0f;
-        t1 = fmaf(gm, u, t1);
-        t2 = fmaf(gm, w, t2);
+        s1 = lanes_sum(s1, l);
+        s2 = lanes_sum(s2, l);
+        if (sub_ == 0 && g == g0) {
+            const float r = a.rstd[q0 + g];
+            k1[g] = s1 * inv * -r;
+            k2[g] = s2 * inv * -r * r;
+        }
     }
-    t1 = warp_sum(t1);
-    t2 = warp_sum(t2);
-    if (lane == 0) { s1[warp] = t1; s2[warp] = t2; }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        const float inv = 1.0f / ((float)a.hw * a.cg);
-        float* const to = a.means + ((size_t)img * a.groups + g) * 2;
-        to[0] = (s1[0] + s1[1] + s1[2] + s1[3]) * inv;
-        to[1] = (s2[0] + s2[1] + s2[2] + s2[3]) * inv;
-    }
-}
-
-template <typename T, int E>
-__global__ void __launch_bounds__(kSplitThreads) back_apply_kernel(const Args a)
-{
-    const Place<E> at(a);
-    let_next_start();
-    wait_for_previous();
-    const size_t g0 = (size_t)at.img * a.groups + at.span * a.gs;
     for (int v = at.v; at.active && v < at.nv; v += kSplitThreads) {
-        Channels<E> par;
-        par.params(a, at.ch0 + v * E);
-        par.stats(a.mean + g0, a.rstd + g0, v * E, a.cg);
-        float k1[E], k2[E];
+        float m[E], g[E], b[E], u[E], w[E];
+        channels<E>(a, at.ch0, v * E, a.mean + q0, a.rstd + q0, m, u, g, b);
+        mul<E>(g, g, u);
+        int q = over(v * E, a.cdiv), next = (q + 1) * a.cg - v * E;
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            k1[j] = a.means[(g0 + (v * E + j) / a.cg) * 2];
-            k2[j] = a.means[(g0 + (v * E + j) / a.cg) * 2 + 1];
+            if (j == next) { ++q; next += a.cg; }
+            u[j] = k1[q];
+            w[j] = k2[q];
         }
-        const size_t first = (size_t)at.img * a.hw * a.c + at.ch0 + v * E;
-        const T* const x = static_cast<const T*>(a.x) + first;
-        const T* const dy = static_cast<const T*>(a.dy) + first;
-        T* const dx = static_cast<T*>(a.out) + first;
-        for (int p = at.p0 + at.r; p < at.p1; p += kBatch / 2 * at.rows) {
-            raw_t<T, E> raw[kBatch / 2], draw[kBatch / 2];
+        const size_t first = ((size_t)at.img * a.hw + at.p0 + at.r) * a.c + at.ch0 + v * E, step = (size_t)at.rows * a.c;
+        const T* x = static_cast<const T*>(a.x) + first;
+        const T* dy = static_cast<const T*>(a.dy) + first;
+        T* dx = static_cast<T*>(a.out) + first;
+        const int loads = (at.p1 - at.p0 - at.r + at.rows - 1) / at.rows;
+        Column<T, E, kDeepBack> col(ring, x, step), dcol(dring, dy, step);
 #pragma unroll
-            for (int i = 0; i < kBatch / 2; ++i)
-                if (p + i * at.rows < at.p1) {
-                    raw[i] = load<T, E>(x + (size_t)(p + i * at.rows) * a.c);
-                    draw[i] = load<T, E>(dy + (size_t)(p + i * at.rows) * a.c);
-                }
+        for (int j = 0; j < kDeepBack; ++j) { col.ask(j, j < loads); dcol.ask(j, j < loads); asked(); }
+        for (int i = 0; i < loads; i += kDeepBack)
 #pragma unroll
-            for (int i = 0; i < kBatch / 2; ++i)
-                if (p + i * at.rows < at.p1) {
-                    float f[E], d[E];
-                    get<T, E>(raw[i], f);
-                    get<T, E>(draw[i], d);
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        const float xh = (f[j] - par.mean[j]) * par.rstd[j];
-                        const float dz = activate_back(fmaf(xh, par.gamma[j], par.beta[j]), d[j], a.act);
-                        f[j] = par.rstd[j] * (fmaf(par.gamma[j], dz, -k1[j]) - xh * k2[j]);
+            for (int j = 0; j < kDeepBack; ++j)
+                if (i + j < loads) {
+                    wait_oldest<kDeepBack>();
+                    float f[E], d[E], z[E];
+                    get<T, E>(col.at(j), f);
+                    get<T, E>(dcol.at(j), d);
+                    sub<E>(f, f, m);
+                    if (SILU || a.relu) {
+                        fma<E>(z, f, g, b);
+                        activate_back<SILU, E>(d, z, a.relu);
                     }
-                    store<T, E>(dx + (size_t)(p + i * at.rows) * a.c, f);
+                    fma<E>(f, f, w, u);
+                    fma<E>(f, d, g, f);
+                    store<T, E>(dx, f);
+                    dx += step;
+                    col.ask(j, i + j + kDeepBack < loads);
+                    dcol.ask(j, i + j + kDeepBack < loads);
+                    asked();
                 }
-        }
     }
 }
 
-// dbeta and dgamma: sums[image][2][channel] over the images, 32 channels per block, eight lanes of images.
-__global__ void __launch_bounds__(256) params_kernel(const float* sums, float* dgamma, float* dbeta, int n, int c)
+// dbeta and dgamma: sums[part][2][channel] over the parts (blocks of images), 8 channels per block (32 bytes of a part), 128 parts side by side.
+__global__ void __launch_bounds__(1024) params_kernel(const float* sums, float* dgamma, float* dbeta, int n, int c)
 {
-    __shared__ float s[2][8][32];
+    __shared__ float s[2][8][129];
     let_next_start();
     wait_for_previous();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, ch = blockIdx.x * 32 + lane;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = threadIdx.x & 7, row = threadIdx.x >> 3, ch = blockIdx.x * 8 + k;
     float u = 0.0f, w = 0.0f;
     if (ch < c)
-#pragma unroll 4
-        for (int i = warp; i < n; i += 8) {
+#pragma unroll 8
+        for (int i = row; i < n; i += 128) {
             u += sums[(size_t)i * 2 * c + ch];
             w += sums[((size_t)i * 2 + 1) * c + ch];
         }
-    s[0][warp][lane] = u;
-    s[1][warp][lane] = w;
+    s[0][k][row] = u;
+    s[1][k][row] = w;
     __syncthreads();
-    if (warp >= 2 || ch >= c) return;
-    float t = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) t += s[warp][k][lane];
-    float* const to = warp ? dgamma : dbeta;
-    if (to) to[ch] = t;
+    if (warp >= 16) return;
+    const float* const from = s[warp >> 3][warp & 7];
+    const float t = warp_sum(from[lane] + from[lane + 32] + (from[lane + 64] + from[lane + 96]));
+    float* const to = warp >> 3 ? dgamma : dbeta;
+    const int out = blockIdx.x * 8 + (warp & 7);
+    if (lane == 0 && out < c && to) to[out] = t;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -723,84 +1002,75 @@ __global__ void __launch_bounds__(256) params_kernel(const float* sums, float* d
 
 struct NormPlan {
     int e;                     // elements per load
-    int gs, threads, loads, cluster, chunk;
-    bool one_pass;
-    int chunks;                // three passes
-    size_t smem;
+    int gs, chunk, loads;
+    int cluster;               // one pass: blocks of a cluster; 0: two passes
+    int chunks;                // blocks per (span, image)
+    size_t smem, ring;         // shared memory of the (first) kernel; two passes: of the second
 };
-
-// The loads a one-pass kernel may hold per thread.
-constexpr int kLoads[2][4] = {{2, 4, 8, 16}, {1, 2, 4, 8}};
-
-int plan_loads(bool back, long long need)
-{
-    for (int v : kLoads[back])
-        if (v >= need) return v;
-    return 0;
-}
 
 int gcd(int a, int b) { return b ? gcd(b, a % b) : a; }
 
-NormPlan make_plan(int n, int hw, int c, int groups, int elt, int align, bool back, int sms)
+NormPlan make_plan(int n, int hw, int c, int groups, int elt, int align, bool back, bool silu, int sms)
 {
     NormPlan p = {};
     const int cg = c / groups;
     p.e = c * elt % 16 == 0 && align % 16 == 0 ? 16 / elt : elt == 2 && c % 4 == 0 && align % 8 == 0 ? 4 : 1;
     int gs0 = p.e / gcd(p.e, cg);                       // groups whose channels are whole loads
-    const int most = kLoads[back][3];
-    auto fits = [&](int gs, int threads, int cluster) {
-        const long long nv = (long long)gs * cg / p.e;
-        return gs <= kMaxSpanGroups && nv <= threads && up_div(up_div(hw, cluster), threads / nv) <= most;
-    };
-    for (int want : {128, 64, 32, 1}) {
-        int gs = gs0;
-        while (gs * 2 <= std::min(kMaxSpanGroups, groups) && gs * cg * elt < want) gs *= 2;
-        gs = std::min(gs, std::max(gs0, groups));
-        for (int threads : {256, 512})
-            for (int cluster = 1; cluster <= 8; cluster *= 2) {
-                if (!fits(gs, threads, cluster)) continue;
-                const long long units = (long long)n * up_div(groups, gs);
-                const int rows = threads / (gs * cg / p.e);
-                while (cluster < 8 && units * cluster * 2 <= 2 * sms && up_div(hw, cluster * 2) >= 2 * rows) cluster *= 2;
-                p.gs = gs; p.threads = threads; p.cluster = cluster;
-                p.chunk = (int)up_div(hw, cluster);
-                p.loads = plan_loads(back, up_div(p.chunk, rows));
-                p.one_pass = true;
-                const size_t nch = (size_t)gs * cg;
-                p.smem = (size_t)threads * p.e * 4 * (back ? 2 : 1) + (back ? 4 * nch * 4 : 0);
-                if (p.smem <= 47 * 1024) return p;
-                p.one_pass = false;
+    // One pass, by what was measured to matter: how much of a sector a span's pixels are, how many blocks of an SM can be in different phases,
+    // how much of a block's time its sums take, how many SMs have work.
+    double best = 0;
+    // The backward pass holds x, dy and, with SiLU, dz: few blocks per SM.  Large calls, which keep the memory busy either way, are faster in two passes
+    // (64 images of 56x56x256, SiLU: 162 us in one pass, 110 in two; 32 of 28x28x256: 21 and 25).
+    for (int gs = gs0; !back || (long long)n * hw * c * elt <= (32 << 20); gs *= 2) {
+        const long long nv = (long long)gs * cg / p.e, nch = up_div((long long)gs * cg, 4) * 4;
+        if (gs > kMaxSpanGroups || gs > std::max(gs0, groups) || nv > kThreads) break;
+        const int rows = (int)(kThreads / nv), bytes = gs * cg * elt;
+        for (int cluster = 1; cluster <= kMaxCluster; cluster *= 2) {
+            const int chunk = (int)up_div(hw, cluster), loads = (int)up_div(chunk, rows);
+            if (cluster > 1 && up_div(hw, chunk) <= cluster / 2) break;
+            const int slots = !back ? 1 : silu && elt == 2 ? 3 : 2;
+            const size_t smem = (size_t)kThreads * p.e * 8 + (back ? 6 : 3) * nch * 4 + (size_t)loads * slots * kThreads * p.e * elt;
+            if (smem > 200 * 1024) continue;
+            const int resident = std::min<int>(back ? 6 : 8, (int)(225 * 1024 / (smem + 1024)));
+            const double blocks = (double)n * up_div(groups, gs) * cluster;
+            const double sector = bytes >= 128 ? 1 : bytes >= 64 ? 0.95 : bytes >= 32 ? 0.8 : 0.5;
+            const double overlap = resident >= 4 ? 1 : resident == 3 ? 0.95 : resident == 2 ? 0.8 : 0.55;
+            const double busy = std::min(1.0, blocks / sms), waves = blocks / (sms * resident);
+            const double tail = waves > 1 ? waves / std::ceil(waves) : 1;
+            const double score = sector * overlap * busy * tail * loads / (loads + (cluster > 8 ? 5.0 : cluster > 1 ? 4.0 : 3.0));
+            if (score > best) {
+                best = score;
+                p.gs = gs; p.cluster = p.chunks = cluster; p.chunk = chunk; p.loads = loads; p.smem = smem;
             }
+        }
     }
-    // Three passes.  A span of more loads than threads has to be one group.
-    p.threads = kSplitThreads;
+    if (best > 0) return p;
+    // Two passes.  A span of more loads than threads has to be one group.
     if ((long long)gs0 * cg / p.e > kSplitThreads && gs0 > 1) { p.e = 1; gs0 = 1; }
     p.gs = gs0;
-    while (p.gs * 2 <= std::min(kMaxSpanGroups, groups) && (long long)p.gs * 2 * cg / p.e <= kSplitThreads && p.gs * cg * elt < 512) p.gs *= 2;
+    while (p.gs * 2 <= std::min(kMaxSpanGroups, groups) && (long long)p.gs * 2 * cg / p.e <= kSplitThreads) p.gs *= 2;
     const long long units = (long long)n * up_div(groups, p.gs);
     const long long nv = (long long)p.gs * cg / p.e, rows = std::max<long long>(1, kSplitThreads / nv);
-    // enough blocks for four per SM, of at least two batches
-    long long chunks = std::min(up_div(4ll * sms, units), up_div(hw, 2 * kBatch * rows));
-    chunks = std::max(1ll, std::min(chunks, 256ll));
-    p.chunk = (int)up_div(hw, chunks);
+    // Long columns of a thread's loads, as far as every SM has work; and short enough for sums of squares less one of the values.
+    const long long loads = std::max(4ll, std::min(32ll, up_div(up_div(hw, rows) * units, 4ll * sms)));
+    p.chunks = (int)std::min(up_div(hw, rows * loads), 4096ll);
+    p.chunk = (int)up_div(hw, p.chunks);
     p.chunks = (int)up_div(hw, p.chunk);
-    p.smem = (size_t)kSplitThreads * p.e * 4 * 2 + (nv <= kSplitThreads ? (size_t)2 * p.gs * cg * 4 : 0);
+    p.ring = (size_t)kSplitThreads * p.e * elt * (back ? 2 * kDeepBack : kDeep);
+    p.smem = ((size_t)kSplitThreads * p.e * 2 + (back ? 4 * up_div((long long)p.gs * cg, 4) * 4 : 0)) * 4 + p.ring;
     return p;
 }
 
-// Of the caller's workspace, in floats: sums [n][2][c]; three passes: means [n][groups][2], part.
+// Of the caller's workspace, in floats: sums [n][blocks of an image][2][c] (backward); two passes: part [n][blocks of an image][groups][2].
 struct Workspace {
-    size_t sums, means, part;
-    size_t bytes() const { return (sums + means + part) * 4; }
+    size_t sums, part;
+    size_t bytes() const { return (sums + part) * 4; }
 };
 Workspace workspace_of(const NormPlan& p, bool back, int n, int c, int groups)
 {
     Workspace w = {};
-    if (back) w.sums = (size_t)n * 2 * c;
-    if (!p.one_pass) {
-        if (back) w.means = (size_t)n * groups * 2;
-        w.part = (size_t)n * p.chunks * 2 * (back ? c : groups);
-    }
+    if (back) w.sums = (size_t)n * p.chunks * 2 * c;
+    if (!p.cluster) w.part = (size_t)n * p.chunks * 2 * groups;
     return w;
 }
 
@@ -808,39 +1078,33 @@ int check_shape(int n, int h, int wd, int c, int groups)
 {
     if (n < 0 || h < 0 || wd < 0 || c < 0 || groups < 1) return ALCS_ERR_INVALID_ARG;
     if (c % groups || c > 65536 || (long long)h * wd >= (1ll << 30) || (long long)n * c >= (1ll << 30)) return ALCS_ERR_SHAPE;
-    return ALCS_OK;
+    return c / groups > kMaxGroupChannels ? ALCS_ERR_UNSUPPORTED : ALCS_OK;
 }
 
 using Kernel = void (*)(const Args);
-template <typename T, int E>
-Kernel one_pass_kernel(bool back, int loads)
-{
-    if (back) return loads == 1 ? norm_back_kernel<T, E, 1> : loads == 2 ? norm_back_kernel<T, E, 2> : loads == 4 ? norm_back_kernel<T, E, 4> : norm_back_kernel<T, E, 8>;
-    return loads == 2 ? norm_kernel<T, E, 2> : loads == 4 ? norm_kernel<T, E, 4> : loads == 8 ? norm_kernel<T, E, 8> : norm_kernel<T, E, 16>;
-}
 // which: 0 one pass, 1 statistics, 2 outputs
 template <typename T, int E>
-Kernel kernel_of(bool back, int which, int loads)
+Kernel kernel_of(bool back, int which, bool silu)
 {
-    if (which == 0) return one_pass_kernel<T, E>(back, loads);
-    if (which == 1) return back ? back_stats_kernel<T, E> : stats_kernel<T, E>;
-    return back ? back_apply_kernel<T, E> : apply_kernel<T, E>;
+    if (which == 0) return back ? (silu ? norm_back_kernel<T, E, true> : norm_back_kernel<T, E, false>) : silu ? norm_kernel<T, E, true> : norm_kernel<T, E, false>;
+    if (which == 1) return back ? (silu ? back_stats_kernel<T, E, true> : back_stats_kernel<T, E, false>) : stats_kernel<T, E>;
+    return back ? (silu ? back_apply_kernel<T, E, true> : back_apply_kernel<T, E, false>) : silu ? apply_kernel<T, E, true> : apply_kernel<T, E, false>;
 }
 template <typename T>
-Kernel kernel_of(int e, bool back, int which, int loads)
+Kernel kernel_of(int e, bool back, int which, bool silu)
 {
-    if (e == 1) return kernel_of<T, 1>(back, which, loads);
+    if (e == 1) return kernel_of<T, 1>(back, which, silu);
     if constexpr (sizeof(T) == 2) {
-        if (e == 4) return kernel_of<T, 4>(back, which, loads);
-        return kernel_of<T, 8>(back, which, loads);
+        if (e == 4) return kernel_of<T, 4>(back, which, silu);
+        return kernel_of<T, 8>(back, which, silu);
     } else {
-        return kernel_of<T, 4>(back, which, loads);
+        return kernel_of<T, 4>(back, which, silu);
     }
 }
-Kernel kernel_of(alcs_dtype dt, const NormPlan& p, bool back, int which)
+Kernel kernel_of(alcs_dtype dt, const NormPlan& p, bool back, int which, bool silu)
 {
-    return dt == ALCS_F32 ? kernel_of<float>(p.e, back, which, p.loads) : dt == ALCS_F16 ? kernel_of<__half>(p.e, back, which, p.loads)
-                                                                                        : kernel_of<__nv_bfloat16>(p.e, back, which, p.loads);
+    return dt == ALCS_F32 ? kernel_of<float>(p.e, back, which, silu) : dt == ALCS_F16 ? kernel_of<__half>(p.e, back, which, silu)
+                                                                                        : kernel_of<__nv_bfloat16>(p.e, back, which, silu);
 }
 
 int align_of(std::initializer_list<const void*> ps)
@@ -851,30 +1115,48 @@ int align_of(std::initializer_list<const void*> ps)
     return align;
 }
 
+// Shared memory beyond 48 KB (with a kernel's own) and clusters of 16, allowed once per kernel and device.
+int allow(const void* fn, size_t smem, int cluster, int dev)
+{
+    static std::mutex mu;
+    static std::set<std::pair<const void*, int>> allowed;
+    if (smem <= 40 * 1024 && cluster <= 8) return ALCS_OK;
+    std::lock_guard<std::mutex> lk(mu);
+    if (allowed.count({fn, dev})) return ALCS_OK;
+    ALCS_CUDA(cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024));
+    ALCS_CUDA(cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    allowed.insert({fn, dev});
+    return ALCS_OK;
+}
+
 int run(Args& a, bool back, alcs_dtype dt, int dev, const NormPlan& p, void* workspace, cudaStream_t st)
 {
     const Workspace w = workspace_of(p, back, a.n, a.c, a.groups);
     a.sums = static_cast<float*>(workspace);
-    a.means = a.sums + w.sums;
-    a.part = a.means + w.means;
+    a.part = a.sums + w.sums;
     a.gs = p.gs;
     a.spans = (int)up_div(a.groups, p.gs);
     a.chunk = p.chunk;
-    a.chunks = p.one_pass ? p.cluster : p.chunks;
+    a.chunks = p.chunks;
+    a.loads = p.loads;
     const long long blocks = (long long)a.n * a.spans * a.chunks;
     if (blocks > 0x7fffffffll) return ALCS_ERR_SHAPE;
+    a.span_ch = (int)up_div((long long)a.gs * a.cg, 4) * 4;
+    a.whole = a.cg % p.e == 0;
+    a.cdiv = tc_div(a.cg);
+    a.vdiv = tc_div(std::max(1, a.cg / p.e));
     const dim3 grid((unsigned)blocks);
-    if (p.one_pass) {
-        ALCS_CUDA(launch_pdl(kernel_of(dt, p, back, 0), grid, p.threads, p.smem, p.cluster, st, a));
-    } else {
-        ALCS_CUDA(launch_pdl(kernel_of(dt, p, back, 1), grid, p.threads, p.smem, 1, st, a));
-        if (back) ALCS_CUDA(launch_pdl(back_unite_kernel, dim3((unsigned)(a.n * a.groups)), 128, 0, 1, st, a));
-        ALCS_CUDA(launch_pdl(kernel_of(dt, p, back, 2), grid, p.threads, p.smem, 1, st, a));
-    }
+    const Kernel first = kernel_of(dt, p, back, p.cluster ? 0 : 1, a.silu);
+    const int rc = allow((const void*)first, p.smem, p.cluster, dev);
+    if (rc) return rc;
+    ALCS_CUDA(launch_pdl(first, grid, p.cluster ? kThreads : kSplitThreads, p.smem, std::max(1, p.cluster), st, a));
+    if (p.cluster) return ALCS_OK;
+    ALCS_CUDA(launch_pdl(kernel_of(dt, p, back, 2, a.silu), grid, kSplitThreads, p.ring, 1, st, a));
     return ALCS_OK;
 }
 
 }  // namespace
+
 }  // namespace alcs
 
 extern "C" {
@@ -884,12 +1166,13 @@ ALCS_API size_t alcs_group_norm_workspace(int n, int h, int wd, int c, int group
     using namespace alcs;
     if (!known_type(dt) || check_shape(n, h, wd, c, groups) || n == 0 || c == 0 || (long long)h * wd == 0) return 0;
     size_t most = 0;
-    // (whatever the alignment of the buffers and the number of SMs)
+    // (whatever the alignment of the buffers and the activation)
     for (int align : {16, 8, 4})
-        for (bool back : {false, true}) {
-            const NormPlan p = make_plan(n, h * wd, c, groups, (int)elt_bytes(dt), align, back, 148);
-            most = std::max(most, workspace_of(p, back, n, c, groups).bytes());
-        }
+        for (bool back : {false, true})
+            for (bool silu : {false, true}) {
+                const NormPlan p = make_plan(n, h * wd, c, groups, (int)elt_bytes(dt), align, back, silu, 148);
+                most = std::max(most, workspace_of(p, back, n, c, groups).bytes());
+            }
     return most;
 }
 
@@ -905,7 +1188,7 @@ ALCS_API int alcs_group_norm(const void* x, void* y, int n, int h, int wd, int c
     const int hw = h * wd;
     if (n == 0 || hw == 0 || c == 0) return ALCS_OK;
     const size_t elt = elt_bytes(dt), bytes = (size_t)n * hw * c * elt, sb = (size_t)n * groups * 4;
-    const NormPlan p = make_plan(n, hw, c, groups, (int)elt, align_of({x, y}), false, 148);
+    const NormPlan p = make_plan(n, hw, c, groups, (int)elt, align_of({x, y}), false, flags & ALCS_SILU, 148);
     const size_t need = workspace_of(p, false, n, c, groups).bytes();
     if (workspace_bytes < need) return ALCS_ERR_INVALID_ARG;
     const Buffer buffers[7] = {{y, bytes, elt, true, false, 1u << 1}, {x, bytes, elt, false, false, 0}, {gamma, (size_t)c * 4, 4, false, true, 0},
@@ -917,7 +1200,7 @@ ALCS_API int alcs_group_norm(const void* x, void* y, int n, int h, int wd, int c
     Args a = {};
     a.x = x; a.out = y; a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd;
     a.n = n; a.hw = hw; a.c = c; a.groups = groups; a.cg = c / groups; a.eps = eps;
-    a.act = flags & ALCS_RELU ? kRelu : flags & ALCS_SILU ? kSilu : kNone;
+    a.relu = (flags & ALCS_RELU) != 0; a.silu = (flags & ALCS_SILU) != 0;
     return run(a, false, dt, dev, p, workspace, static_cast<cudaStream_t>(cuda_stream));
 }
 
@@ -938,7 +1221,7 @@ ALCS_API int alcs_group_norm_backward(const void* x, const void* dy, void* dx, i
     NormPlan p = {};
     size_t need = 0;
     if (!none) {
-        p = make_plan(n, hw, c, groups, (int)elt, align_of({x, dy, dx}), true, 148);
+        p = make_plan(n, hw, c, groups, (int)elt, align_of({x, dy, dx}), true, flags & ALCS_SILU, 148);
         need = workspace_of(p, true, n, c, groups).bytes();
         if (workspace_bytes < need) return ALCS_ERR_INVALID_ARG;
     }
@@ -954,12 +1237,12 @@ ALCS_API int alcs_group_norm_backward(const void* x, const void* dy, void* dx, i
         Args a = {};
         a.x = x; a.dy = dy; a.out = dx; a.gamma = gamma; a.beta = beta; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
         a.n = n; a.hw = hw; a.c = c; a.groups = groups; a.cg = c / groups;
-        a.act = flags & ALCS_RELU ? kRelu : flags & ALCS_SILU ? kSilu : kNone;
+        a.relu = (flags & ALCS_RELU) != 0; a.silu = (flags & ALCS_SILU) != 0;
         rc = run(a, true, dt, dev, p, workspace, st);
         if (rc) return rc;
     }
     if (dgamma || dbeta)
-        ALCS_CUDA(launch_pdl(params_kernel, dim3((unsigned)up_div(c, 32)), 256, 0, 1, st, static_cast<const float*>(workspace), dgamma, dbeta, none ? 0 : n, c));
+        ALCS_CUDA(launch_pdl(params_kernel, dim3((unsigned)up_div(c, 8)), 1024, 0, 1, st, static_cast<const float*>(workspace), dgamma, dbeta, none ? 0 : n * p.chunks, c));
     return ALCS_OK;
 }
 

@@ -30,11 +30,12 @@ REFUSED = [
     ("alcs_group_norm", NORM, dict(n=-1), INVALID), ("alcs_group_norm", NORM, dict(h=-1), INVALID), ("alcs_group_norm", NORM, dict(c=-8), INVALID),
     ("alcs_group_norm", NORM, dict(groups=0), INVALID), ("alcs_group_norm", NORM, dict(groups=7), SHAPE),
     ("alcs_group_norm", NORM, dict(c=1 << 17, groups=1 << 10), SHAPE), ("alcs_group_norm", NORM, dict(h=1 << 15, wd=1 << 15), SHAPE),
+    ("alcs_group_norm", NORM, dict(c=8256, groups=1), -3), ("alcs_group_norm_backward", BACK, dict(c=16400, groups=2), -3),
     ("alcs_group_norm", NORM, dict(n=1 << 24), SHAPE), ("alcs_group_norm", NORM, dict(eps=-1.0), INVALID),
     ("alcs_group_norm", NORM, dict(eps=float("nan")), INVALID), ("alcs_group_norm", NORM, dict(eps=float("inf")), INVALID),
     ("alcs_group_norm", NORM, dict(flags=2), INVALID), ("alcs_group_norm", NORM, dict(flags=5), INVALID), ("alcs_group_norm", NORM, dict(flags=8), INVALID),
     ("alcs_group_norm", NORM, dict(dt=3), INVALID), ("alcs_group_norm", NORM, dict(dt=-1), INVALID),
-    # a shape of three passes without its workspace
+    # a shape of two passes without its workspace
     ("alcs_group_norm", NORM, dict(h=512, wd=512, y=1 << 32, gamma=None, beta=None), INVALID),
     ("alcs_group_norm_backward", BACK, dict(dy=None), INVALID), ("alcs_group_norm_backward", BACK, dict(dx=None), INVALID),
     ("alcs_group_norm_backward", BACK, dict(mean=None), INVALID), ("alcs_group_norm_backward", BACK, dict(rstd=None), INVALID),
@@ -100,8 +101,8 @@ def test_sizes(alcs):
 
 
 def test_workspace_of_group_norm(alcs):
-    """Two sums per channel and image; more where three passes are needed; nothing for nothing."""
-    assert alcs.alcs_group_norm_workspace(2, 7, 7, 64, 8, alcs.ALCS_BF16) == 2 * 2 * 64 * 4
+    """At least two sums per channel and image; more where an image is spread over blocks; nothing for nothing."""
+    assert alcs.alcs_group_norm_workspace(2, 7, 7, 64, 8, alcs.ALCS_BF16) >= 2 * 2 * 64 * 4
     assert alcs.alcs_group_norm_workspace(1, 512, 512, 64, 8, alcs.ALCS_F32) > 2 * 64 * 4
     for args in ((0, 7, 7, 64, 8, 0), (2, 0, 7, 64, 8, 0), (2, 7, 7, 0, 8, 0), (2, 7, 7, 64, 0, 0), (2, 7, 7, 64, 7, 0), (2, 7, 7, 64, 8, 5), (-2, 7, 7, 64, 8, 0)):
         assert alcs.alcs_group_norm_workspace(*args) == 0

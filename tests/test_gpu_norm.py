@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from dense_util import back_bounds, f64, flags_of, norm_bound, types
+from dense_util import HALF, back_bounds, f64, flags_of, norm_bound, types
 from oracle import dense
 
 pytestmark = pytest.mark.gpu
@@ -22,6 +22,13 @@ def _inputs(seed, n, hw, c, dtype, alcs, mean=0.5, spread=1.0):
     t = types(alcs)[dtype][1]
     x = (rnd(n, hw, c) * spread + mean * rnd(c)).to(t)
     return x, rnd(n, hw, c).to(t), 1 + 0.3 * rnd(c), 0.3 * rnd(c)
+
+
+# Calls large enough to read x twice from L2: images of several runs and of one, more images than stay in L2, loads of 16, 8 and 2 or 4 bytes, threads without
+# channels, one row of pixels at a time, one image
+LARGE = [(16, 56, 56, 256, 32, "bf16", "silu"), (16, 56, 56, 256, 32, "f16", "relu"), (40, 62, 63, 100, 10, "f16", "none"), (24, 50, 56, 150, 30, "f32", "silu"),
+         (8, 28, 28, 2048, 32, "bf16", "silu"), (1, 448, 448, 64, 8, "f32", "silu"), (600, 9, 16, 320, 64, "bf16", "none"), (90, 20, 20, 380, 76, "f16", "silu"),
+         (50, 64, 64, 31, 31, "f32", "relu")]
 
 
 class Norm:
@@ -80,6 +87,48 @@ def test_forward_and_backward(alcs, shape, dtype, act):
     xa = np.abs(f64(x)).reshape(n, h * w, groups, -1)
     _within(f64(k.mean), ref["mean"], 64 * 2.0 ** -24 * xa.mean((1, 3)) + 1e-30)
     _within(f64(k.rstd), ref["rstd"], 128 * 2.0 ** -24 * ref["rstd"] * (1 + xa.max((1, 3)) * ref["rstd"] * 1e-3))
+
+
+@pytest.mark.parametrize("case", LARGE, ids=lambda s: "x".join(map(str, s)))
+def test_large_calls(alcs, case):
+    """Every image against the definition for the first and last ones, the others by what the sums over all of them are."""
+    import torch
+    *shape, dtype, act = case
+    n, h, w, c, groups = shape
+    x, dy, gamma, beta = _inputs(sum(shape), n, h * w, c, dtype, alcs)
+    k = Norm(alcs, x, tuple(shape), dtype, act, 1e-5, gamma, beta)
+    y, dx = k.forward(), k.backward(dy)
+    assert alcs.alcs_dense_status() == 0
+    xd, g64, b64 = x.double().view(n, h * w, groups, -1), gamma.double(), beta.double()
+    mean = xd.mean((1, 3), keepdim=True)
+    rstd = 1 / ((xd - mean).square().mean((1, 3), keepdim=True) + 1e-5).sqrt()
+    xh = ((xd - mean) * rstd).view(n, h * w, c)
+    z = xh * g64 + b64
+    s = torch.sigmoid(z)
+    slope = s + z * s * (1 - s) if act == "silu" else (z > 0).double() if act == "relu" else torch.ones_like(z)
+    ref_y = z * s if act == "silu" else z.clamp(min=0) if act == "relu" else z
+    dz = dy.double() * slope
+    t = (dz * g64).view(n, h * w, groups, -1)
+    xg = xh.view(n, h * w, groups, -1)
+    ref_dx = (rstd * (t - t.mean((1, 3), keepdim=True) - xg * (t * xg).mean((1, 3), keepdim=True))).view(n, h * w, c)
+    # the bounds of dense_util, image by image
+    for i in sorted({0, 1 % n, n // 2, n - 1}):
+        ref = dense.group_norm_backward(f64(x[i:i + 1]), f64(dy[i:i + 1]), groups, f64(gamma), f64(beta), 1e-5, act)
+        assert np.abs(f64(ref_dx[i:i + 1]) - ref["dx"]).max() < 1e-9 and np.abs(f64(ref_y[i:i + 1]) - ref["y"]).max() < 1e-9
+        _within(f64(y[i:i + 1]), ref["y"], norm_bound(ref, f64(x[i:i + 1]), f64(gamma), f64(beta), groups, dtype))
+        if act != "relu":
+            _within(f64(dx[i:i + 1]), ref["dx"], back_bounds(ref, f64(x[i:i + 1]), f64(dy[i:i + 1]), f64(gamma), f64(beta), groups, dtype)[0])
+    # all of them, by the sum of squared differences: each is at most the bound, which is a few units of the type in the mean
+    for got, ref in ((y, ref_y), (dx, ref_dx)):
+        d = (got.double() - ref).norm() / ref.norm()
+        # relu: a slope of the wrong side where z is within 64 u (1 + M) of 0, at most one value in 10^4, each off by less than 10 of them
+        assert d < HALF[dtype] + 256 * 2.0 ** -24 + (0.02 if act == "relu" and got is dx else 0), d.item()
+    # sums of n h w values: 64 u of their magnitudes, and what dz and xh themselves are off by (1e-5, with M of 10 or less)
+    for got, term in ((k.dgamma, dz * xh), (k.dbeta, dz)):
+        ref, scale = term.sum((0, 1)), term.abs().sum((0, 1))
+        assert ((got.double() - ref).abs() <= 2e-5 * scale + (1e-4 * dy.double().abs().sum((0, 1)) if act == "relu" else 0)).all()
+    # the same bits again
+    assert (k.forward() == y).all() and (k.backward(dy) == dx).all()
 
 
 @pytest.mark.parametrize("shape", [(2, 14, 14, 128, 8), (1, 130, 120, 64, 2)])
