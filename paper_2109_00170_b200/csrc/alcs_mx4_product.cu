@@ -26,13 +26,14 @@ namespace {
 
 constexpr int kEpiWarps = 8, kLoadWarp = 8, kMmaWarp = 9;
 constexpr int kThreads = 320;
-constexpr int kStageBlocks = 4;                         // blocks of 32 columns per stage: one group of scales
-constexpr int kMaxN = 256, kAccCols = 384;              // tensor memory: accumulators, then 12 columns of scales per stage
+constexpr int kQuads = 2;                               // a stage: up to so many groups of four blocks of 32 columns
+constexpr int kMaxN = 256;
+constexpr int kSlots = 3, kSlotCols = 128;              // tensor memory: accumulators of 128 columns, a tile has one or two; then scales, 12 columns per group
 constexpr int kMaxStages = 8;
-constexpr int kHeader = 1024, kStaging = 32 * 128;      // shared memory: barriers; a 32 x 32 piece of the output per epilogue warp
+constexpr int kBias = 1024, kHeader = kBias + 8 * 256, kStaging = 32 * 128;      // shared memory: barriers; per epilogue warp: bias, a 32 x 32 piece of the output
 constexpr int kMaxSplit = 8;
 constexpr int kScaleBytes = 512;
-static_assert(kAccCols + 12 * kMaxStages <= 512, "tensor memory");
+constexpr int kScaleCols = 512 - kSlots * kSlotCols;
 
 __device__ int g_error;      // see alcs_dense_status
 
@@ -45,9 +46,10 @@ struct Args {
     Operand a, b;               // rows and columns of a tile
     int blocks, quads;          // blocks of 32 columns as stored (even), groups of four
     int n;                      // columns of a tile: 64, 128, 192, 256, or the only tile's, a multiple of 16
-    int tiles_b;
-    long long tiles;
-    int split, stages, stage_bytes;
+    int tiles;
+    TcDiv tiles_b;
+    int split, stages;
+    int stage_quads, tile_bytes, stage_bytes;      // of a stage: groups; 128 rows of one operand; all
     int cout;                   // of y's row
     int swapped;                // a is the weights
     int relu, vec;              // vec: rows of y (and the residual) are whole 16 bytes
@@ -94,25 +96,41 @@ __device__ __forceinline__ void store_one(const Args& a, size_t at, float v, flo
     from_f32(static_cast<T*>(a.y) + at, v);
 }
 
+// max(v, 0) of packed values, NaN to 0 (of rounded values: the rounding keeps their sign)
+__device__ __forceinline__ unsigned positive(unsigned v, __half)
+{
+    const __half2 z = __hmax2(reinterpret_cast<const __half2&>(v), __float2half2_rn(0.0f));
+    return reinterpret_cast<const unsigned&>(z);
+}
+__device__ __forceinline__ unsigned positive(unsigned v, __nv_bfloat16)
+{
+    const __nv_bfloat162 z = __hmax2(reinterpret_cast<const __nv_bfloat162&>(v), __float2bfloat162_rn(0.0f));
+    return reinterpret_cast<const unsigned&>(z);
+}
+__device__ __forceinline__ unsigned positive(unsigned v, float) { return __float_as_uint(fmaxf(__uint_as_float(v), 0.0f)); }
+template <typename T>
+__device__ __forceinline__ uint4 positive(const uint4& v, T t) { return make_uint4(positive(v.x, t), positive(v.y, t), positive(v.z, t), positive(v.w, t)); }
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
 {
     extern __shared__ __align__(1024) unsigned char smem[];
     const unsigned base = smem_u32(smem);
-    const unsigned full = base, empty = base + 8 * kMaxStages, acc_full = empty + 8 * kMaxStages, acc_empty = acc_full + 8 * 8, drained = acc_empty + 8 * 8;
+    const unsigned full = base, empty = base + 8 * kMaxStages, acc_full = empty + 8 * kMaxStages, acc_empty = acc_full + 8 * kSlots, drained = acc_empty + 8 * kSlots;
     const unsigned tmem_slot = drained + 8;
     const unsigned staging0 = base + kHeader, stage0 = staging0 + kEpiWarps * kStaging;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int S = a.stages, n = a.n, n_acc = min(8, kAccCols / ((n + 31) / 32 * 32));
-    const unsigned acc_cols = (unsigned)((n + 31) / 32 * 32);
+    const int S = a.stages, n = a.n, Q = a.stage_quads;
+    const unsigned halves = n > kSlotCols ? 2 : 1;
     const unsigned rank = a.split > 1 ? cluster_rank() : 0;
-    const long long first_tile = blockIdx.x / a.split, tile_step = gridDim.x / a.split;
-    // this block's share of the columns, in groups of four blocks
-    const int q0 = (int)((long long)a.quads * rank / a.split), q1 = (int)((long long)a.quads * (rank + 1) / a.split);
+    const int first_tile = blockIdx.x / a.split, tile_step = gridDim.x / a.split;
+    // this block's share of the columns, in stages
+    const int steps_all = Q ? (a.quads + Q - 1) / Q : 0;
+    const int q0 = (int)((long long)steps_all * rank / a.split), q1 = (int)((long long)steps_all * (rank + 1) / a.split);
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kMaxStages; ++i) { bar_init(full + 8 * i, 1); bar_init(empty + 8 * i, 1); }
-        for (int i = 0; i < 8; ++i) { bar_init(acc_full + 8 * i, 1); bar_init(acc_empty + 8 * i, kEpiWarps); }
+        for (int i = 0; i < kSlots; ++i) { bar_init(acc_full + 8 * i, 1); bar_init(acc_empty + 8 * i, kEpiWarps); }
         bar_init(drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -131,37 +149,28 @@ __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
     bool ok = true;
     if (warp == kLoadWarp) {
         unsigned stage = 0, ph = 1, used = 0;
-        const int pitch = n * 16;      // bytes of a block's rows of b in shared memory
 #pragma unroll 1
-        for (long long t = first_tile; t < a.tiles && ok; t += tile_step) {
-            const int ta = (int)(t / a.tiles_b), tb = (int)(t - (long long)ta * a.tiles_b);
-            const int r0 = tb * n, r1 = min(r0 + n, a.b.tiles * 128);      // rows of b that exist (those behind b.rows hold anything)
-            const int t0 = r0 >> 7, nt = (r1 - 1 >> 7) - t0 + 1;           // its tiles of 128 rows: 1 to 3
+        for (int t = first_tile; t < a.tiles && ok; t += tile_step) {
+            const int ta = div_of(t, a.tiles_b), tb = t - ta * a.tiles_b.d;
+            // whole tiles of 128 rows of b, one or two: fewer copies are worth more than the rows of neighbours
+            const int t0 = tb * a.n >> 7, nt = (min(tb * a.n + a.n, a.b.tiles * 128) - 1 >> 7) - t0 + 1;
+            // lanes: the rows of a; of b's tiles; the scales of a; of b's tiles
+            const int which = lane <= nt ? 0 : 1, at_tile = lane <= nt ? lane : lane - nt - 1;
+            const Operand& op = at_tile == 0 ? a.a : a.b;
+            const size_t tile = at_tile == 0 ? ta : t0 + at_tile - 1;
+            const unsigned char* from = which ? op.scales + tile * a.quads * kScaleBytes : op.data + tile * a.blocks * 2048;
+            const unsigned to = (which ? (unsigned)(a.stage_bytes - 3 * Q * kScaleBytes) + at_tile * Q * kScaleBytes : at_tile * a.tile_bytes) + stage0;
 #pragma unroll 1
             for (int q = q0; q < q1 && ok; ++q) {
-                const int nb = min(kStageBlocks, a.blocks - q * kStageBlocks);
+                const int nb = min(4 * Q, a.blocks - q * 4 * Q), nq = min(Q, a.quads - q * Q);
                 ok = __all_sync(0xffffffffu, bar_wait(empty + 8 * stage, ph));
                 if (!ok) break;
-                const unsigned bar = full + 8 * stage, at = stage0 + stage * a.stage_bytes;
+                const unsigned bar = full + 8 * stage;
                 if (lane == 0)
-                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;"
-                                 ::"r"(bar), "r"((unsigned)(nb * (2048 + (r1 - r0) * 16) + (1 + nt) * kScaleBytes)) : "memory");
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"((unsigned)((1 + nt) * (nb * 2048 + nq * kScaleBytes))) : "memory");
                 __syncwarp();
-                // lanes 0 .. 11: rows of b; then the rows of a, the scales of both
-                const unsigned to_b = at + 8192, to_s = to_b + kStageBlocks * pitch;
-                if (lane < 12) {
-                    const int b = lane & 3, i = lane >> 2;
-                    const int s0 = max(r0, (t0 + i) * 128), s1 = min(r1, (t0 + i + 1) * 128);
-                    if (b < nb && s0 < s1)
-                        bulk_load(to_b + b * pitch + (s0 - r0) * 16, a.b.data + (((size_t)(t0 + i) * a.blocks + q * kStageBlocks + b) * 128 + (s0 & 127)) * 16,
-                                  (unsigned)(s1 - s0) * 16, bar);
-                } else if (lane == 12) {
-                    bulk_load(at, a.a.data + ((size_t)ta * a.blocks + q * kStageBlocks) * 2048, (unsigned)nb * 2048, bar);
-                } else if (lane == 13) {
-                    bulk_load(to_s, a.a.scales + ((size_t)ta * a.quads + q) * kScaleBytes, kScaleBytes, bar);
-                } else if (lane < 14 + nt) {
-                    bulk_load(to_s + (lane - 13) * kScaleBytes, a.b.scales + ((size_t)(t0 + lane - 14) * a.quads + q) * kScaleBytes, kScaleBytes, bar);
-                }
+                if (lane < 2 + 2 * nt)
+                    bulk_load(to + stage * a.stage_bytes, from + (size_t)q * (which ? Q * kScaleBytes : a.tile_bytes), which ? nq * kScaleBytes : nb * 2048, bar);
                 ++used;
                 if (++stage == (unsigned)S) { stage = 0; ph ^= 1u; }
             }
@@ -175,38 +184,58 @@ __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
         if (!ok) atomicExch(&g_error, 2);
     } else if (warp == kMmaWarp) {
         if (elect_one()) {
-            unsigned stage = 0, ph = 0, acc = 0, acc_ph = 1;
+            unsigned stage = 0, ph = 0, acc = 0, acc_ph = 1;      // (a slot's phase turns when the ring has)
             // E2M1 x E2M1 (type 1 each), scales E8M0; N / 8 at bit 17, M / 128 at bit 27
-            const unsigned idesc = (1u << 7) | (1u << 10) | ((unsigned)(n >> 3) << 17) | (1u << 23) | (1u << 27);
-            // K-major, no swizzle: blocks of 32 columns 2048 (b: 16 n) bytes apart, groups of 8 rows 128 bytes
-            const unsigned long long da = (128ull << 16) | (8ull << 32) | (1ull << 46), db = ((unsigned long long)n << 16) | (8ull << 32) | (1ull << 46);
-            const unsigned long long ds = (8ull << 16) | (8ull << 32) | (1ull << 46);
+            const unsigned idesc = (1u << 7) | (1u << 10) | (1u << 23) | (1u << 27);
+            // K-major, no swizzle: blocks of 32 columns 2048 bytes apart, groups of 8 rows 128 bytes
+            const unsigned long long dm = (128ull << 16) | (8ull << 32) | (1ull << 46), ds = (8ull << 16) | (8ull << 32) | (1ull << 46);
 #pragma unroll 1
-            for (long long t = first_tile; t < a.tiles && ok; t += tile_step) {
-                const int tb = (int)(t % a.tiles_b);
-                const unsigned shift = (unsigned)(tb * n & 127) >> 5;      // where row 0 of the tile stands in its first 128 rows' scales
+            for (int t = first_tile; t < a.tiles && ok; t += tile_step) {
+                const int tb = t - div_of(t, a.tiles_b) * a.tiles_b.d;
+                // the columns that are rows of b's first tile, and of its second
+                const unsigned off = (unsigned)(tb * n & 127), n0 = min((unsigned)n, 128 - off), n1 = n - n0;
                 const int nt = (min(tb * n + n, a.b.tiles * 128) - 1 >> 7) - (tb * n >> 7) + 1;
-                const unsigned d = tmem + acc * acc_cols;
-                ok = bar_wait(acc_empty + 8 * acc, acc_ph);
+                unsigned d[2], bar[2];
+                for (unsigned h = 0; h < halves; ++h) {
+                    d[h] = tmem + acc * kSlotCols;
+                    bar[h] = acc_full + 8 * acc;
+                    ok = ok && bar_wait(acc_empty + 8 * acc, acc_ph);
+                    if (++acc == kSlots) { acc = 0; acc_ph ^= 1u; }
+                }
 #pragma unroll 1
                 for (int q = q0; q < q1 && ok; ++q) {
                     ok = bar_wait(full + 8 * stage, ph);
                     if (!ok) break;
                     tc_after();
-                    const unsigned at = stage0 + stage * a.stage_bytes, to_b = at + 8192, to_s = to_b + kStageBlocks * n * 16;
-                    const unsigned sa = tmem + kAccCols + 12 * stage, sb = sa + 4;
-                    scales_to_tmem(sa, ds | field(to_s));
+                    const unsigned at = stage0 + stage * a.stage_bytes, to_s = at + a.stage_bytes - 3 * Q * kScaleBytes;
+                    const int nq = min(Q, a.quads - q * Q);
 #pragma unroll 1
-                    for (int i = 0; i < nt; ++i) scales_to_tmem(sb + 4 * i, ds | field(to_s + (1 + i) * kScaleBytes));
-                    const int steps = min(kStageBlocks, a.blocks - q * kStageBlocks) / 2;
+                    for (int g = 0; g < nq; ++g) {
+                        const unsigned sa = tmem + kSlots * kSlotCols + 12 * (stage * Q + g), sb = sa + 4;
+                        for (int i = 0; i <= nt; ++i) scales_to_tmem(sa + 4 * i, ds | field(to_s + (i * Q + g) * kScaleBytes));
+                        const int steps = min(4, a.blocks - (q * Q + g) * 4) / 2;
 #pragma unroll 1
-                    for (int k = 0; k < steps; ++k)      // two blocks each; bits 4 and 29: which bytes of the scales
-                        mma_mx4(d, da | field(at + k * 4096), db | field(to_b + k * n * 32), idesc | (unsigned)k << 5 | (unsigned)k << 30, sa, sb + shift, q > q0 || k > 0);
+                        for (int k = 0; k < steps; ++k) {      // two blocks each; bits 4 and 29: which bytes of the scales
+                            const unsigned id = idesc | (unsigned)k << 5 | (unsigned)k << 30, acc_in = q > q0 || g > 0 || k > 0;
+                            const unsigned col = at + (g * 4 + k * 2) * 2048;
+                            const unsigned first = at + a.tile_bytes + (g * 4 + k * 2) * 2048 + off * 16;
+                            const unsigned m0 = min(n0, 128u), m1 = n - m0;      // columns of the two accumulators
+                            // (a tile that starts in the middle of 128 rows: its accumulators' border is not that of the tiles of rows)
+                            if (off == 0 || n1 == 0 || nt == 1) {
+                                mma_mx4(d[0], dm | field(col), dm | field(first), id | (m0 >> 3) << 17, sa, sb + (off >> 5), acc_in);
+                                if (m1 && nt > 1) mma_mx4(d[1], dm | field(col), dm | field(first - off * 16 + a.tile_bytes), id | (m1 >> 3) << 17, sa, sb + 4, acc_in);
+                            } else {      // 64 rows of the first, 64 and 64 of the second
+                                mma_mx4(d[0], dm | field(col), dm | field(first), id | 8u << 17, sa, sb + 2, acc_in);
+                                mma_mx4(d[0] + 64, dm | field(col), dm | field(first - off * 16 + a.tile_bytes), id | 8u << 17, sa, sb + 4, acc_in);
+                                mma_mx4(d[1], dm | field(col), dm | field(first - off * 16 + a.tile_bytes + 64 * 16), id | 8u << 17, sa, sb + 6, acc_in);
+                            }
+                        }
+                    }
                     mma_commit(empty + 8 * stage);
                     if (++stage == (unsigned)S) { stage = 0; ph ^= 1u; }
                 }
-                if (ok) mma_commit(acc_full + 8 * acc);
-                if (++acc == (unsigned)n_acc) { acc = 0; acc_ph ^= 1u; }
+                if (ok)
+                    for (unsigned h = 0; h < halves; ++h) mma_commit(bar[h]);
             }
             if (!ok) {      // gave up: see the MMAs in flight end before tensor memory is given back
                 mma_commit(drained);
@@ -217,107 +246,122 @@ __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
         __syncwarp();
     } else {
         const int quarter = warp & 3, half = warp >> 2;
-        const unsigned staging = staging0 + warp * kStaging;
+        const unsigned staging = staging0 + warp * kStaging, bias_at = base + kBias + warp * 256;
+        constexpr int W = Pack<T>::n, L = 32 / W;      // elements of a store; lanes of a row, and stores of a piece
         unsigned acc = 0, acc_ph = 0;
 #pragma unroll 1
-        for (long long t = first_tile; t < a.tiles && ok; t += tile_step) {
-            const int ta = (int)(t / a.tiles_b), tb = (int)(t - (long long)ta * a.tiles_b);
-            float v[4][32];
-            ok = __all_sync(0xffffffffu, bar_wait(acc_full + 8 * acc, acc_ph));
-            if (!ok) break;
-            tc_after();
-            const unsigned from = tmem + acc * acc_cols + ((unsigned)quarter << 21);
+        for (int t = first_tile; t < a.tiles && ok; t += tile_step) {
+            const int ta = div_of(t, a.tiles_b), tb = t - ta * a.tiles_b.d;
+            if (a.res && !a.swapped && ta * 128 + quarter * 32 + lane < a.a.rows)      // on its way while the tile is multiplied
+                for (int c = tb * n; c < min(tb * n + n, a.cout); c += 128 / (int)sizeof(T))
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const T*>(a.res) + (size_t)(ta * 128 + quarter * 32 + lane) * a.cout + c));
+#pragma unroll 1
+            for (unsigned h = 0; h < halves && ok; ++h) {
+                // the warp's pieces of this half: columns 0 and 64 of it (or 32 and 96), 32 each
+                const int piece0 = tb * n + (int)h * kSlotCols + half * 32, end = min(tb * n + n, a.swapped ? a.b.tiles * 128 : a.b.rows);
+                float bias[2] = {0.0f, 0.0f};      // of a lane's column of each
+                if (a.bias && !a.swapped)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if ((2 * i + half) * 32 < n) tmem_ld32(from + (2 * i + half) * 32, v[i]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tmem_wait_ld(v[i]);
-            if (q0 == q1)      // no columns: nothing was multiplied
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) v[i][j] = 0.0f;
-            tc_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive(acc_empty + 8 * acc);
-            if (++acc == (unsigned)n_acc) { acc = 0; acc_ph ^= 1u; }
-            const int row = quarter * 32 + lane;      // of the tile
-            if (a.split > 1) {
-                // partial sums to shared memory, where the stages were: swapped [column][128], else [row][n + 1] (no bank twice)
-                float* const part = reinterpret_cast<float*>(smem + (stage0 - base));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int c0 = (2 * i + half) * 32;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (c0 + j < n) part[a.swapped ? (c0 + j) * 128 + row : row * (n + 1) + c0 + j] = v[i][j];
-                }
-                break;
-            }
-            if (a.swapped) {      // a lane has a channel: 32 neighbours of a pixel's row at a time
-                const int c = ta * 128 + row;
-                if (c < a.a.rows) {
-                    const float bias = a.bias ? __ldg(a.bias + c) : 0.0f;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const int p = tb * n + (2 * i + half) * 32 + j;
-                            if ((2 * i + half) * 32 + j < n && p < a.b.rows) store_one<T>(a, (size_t)p * a.cout + c, v[i][j], bias);
-                        }
-                }
-                continue;
-            }
-            // a lane has a pixel: a piece of 32 channels goes through shared memory, so that neighbouring lanes store neighbouring bytes
-            constexpr int W = Pack<T>::n, L = 32 / W;      // elements of a store, lanes of a row
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c0 = tb * n + (2 * i + half) * 32, c1 = min(min(c0 + 32, tb * n + n), a.b.rows);
-                if (c0 >= c1) continue;
+                    for (int i = 0; i < 2; ++i)
+                        if (piece0 + 64 * i + lane < end) bias[i] = __ldg(a.bias + piece0 + 64 * i + lane);
+                float v[2][32];
+                ok = __all_sync(0xffffffffu, bar_wait(acc_full + 8 * acc, acc_ph));
+                if (!ok) break;
+                tc_after();
+                const unsigned from = tmem + acc * kSlotCols + ((unsigned)quarter << 21) + half * 32;
+                tmem_ld32(from, v[0]);
+                tmem_ld32(from + 64, v[1]);
+                tmem_wait_ld(v[0]);
+                tmem_wait_ld(v[1]);
+                tc_before();
                 __syncwarp();
+                if (lane == 0) bar_arrive(acc_empty + 8 * acc);
+                if (++acc == kSlots) { acc = 0; acc_ph ^= 1u; }
+                if (q0 == q1)      // no columns: nothing was multiplied
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(staging + lane * 128 + ((j ^ (lane & 7)) << 4)), "f"(v[i][4 * j]), "f"(v[i][4 * j + 1]),
-                                 "f"(v[i][4 * j + 2]), "f"(v[i][4 * j + 3]) : "memory");
-                __syncwarp();
-                const int c = c0 + lane % L * W;
-                if (a.vec) {
-                    float bias[W];
+                    for (int j = 0; j < 32; ++j) v[0][j] = v[1][j] = 0.0f;
+                const int row = quarter * 32 + lane;      // of the tile
+                if (a.split > 1) {
+                    // partial sums to shared memory, where the stages were: swapped [column][128], else [row][n + 1] (no bank twice)
+                    float* const part = reinterpret_cast<float*>(smem + (stage0 - base));
 #pragma unroll
-                    for (int j = 0; j < W; ++j) bias[j] = a.bias && c + j < c1 ? __ldg(a.bias + c + j) : 0.0f;
+                    for (int i = 0; i < 2; ++i) {
+                        const int c0 = (int)h * kSlotCols + half * 32 + 64 * i;
 #pragma unroll
-                    for (int k = 0; k < L; ++k) {
-                        const int r = k * W + lane / L;      // (32 / L = W rows at a time)
-                        const int p = ta * 128 + quarter * 32 + r;
-                        float o[W];
+                        for (int j = 0; j < 32; ++j)
+                            if (c0 + j < n) part[a.swapped ? (c0 + j) * 128 + row : row * (n + 1) + c0 + j] = v[i][j];
+                    }
+                    continue;
+                }
+                if (a.swapped) {      // a lane has a channel: 32 neighbours of a pixel's row at a time
+                    const int c = ta * 128 + row;
+                    if (c < a.a.rows) {
+                        const float b = a.bias ? __ldg(a.bias + c) : 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) {
+                                const int p = piece0 + 64 * i + j;
+                                if (p < tb * n + n && p < a.b.rows) store_one<T>(a, (size_t)p * a.cout + c, v[i][j], b);
+                            }
+                    }
+                    continue;
+                }
+                // a lane has a pixel: a piece of 32 channels goes through shared memory, so that neighbouring lanes store neighbouring bytes
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int c0 = piece0 + 64 * i;
+                    if (c0 >= end) continue;
+                    __syncwarp();
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(bias_at + lane * 4), "f"(bias[i]) : "memory");
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(staging + lane * 128 + ((j ^ (lane & 7)) << 4)), "f"(v[i][4 * j]), "f"(v[i][4 * j + 1]),
+                                     "f"(v[i][4 * j + 2]), "f"(v[i][4 * j + 3]) : "memory");
+                    __syncwarp();
+                    const int r0 = ta * 128 + quarter * 32;      // the piece's first pixel
+                    if (a.vec) {
+                        const int c = c0 + lane % L * W, most = c < end ? a.a.rows - r0 - lane / L : 0;      // rows from the lane's first on
+                        const size_t at = (size_t)(r0 + lane / L) * a.cout + c, step = (size_t)W * a.cout;      // (32 / L = W rows at a time)
+                        uint4 res[L];
+                        if (a.res)
+#pragma unroll
+                            for (int k = 0; k < L; ++k)
+                                if (k * W < most) res[k] = *reinterpret_cast<const uint4*>(static_cast<const T*>(a.res) + at + k * step);
+                        float b[W];
 #pragma unroll
                         for (int j = 0; j < W; j += 4)
-                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o[j]), "=f"(o[j + 1]), "=f"(o[j + 2]), "=f"(o[j + 3])
-                                         : "r"(staging + r * 128 + (((lane % L * W + j) / 4 ^ (r & 7)) << 4)) : "memory");
-                        if (p >= a.a.rows || c >= c1) continue;
-                        const size_t at = (size_t)p * a.cout + c;
+                            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b[j]), "=f"(b[j + 1]), "=f"(b[j + 2]), "=f"(b[j + 3])
+                                         : "r"(bias_at + (lane % L * W + j) * 4) : "memory");
+                        T* y = static_cast<T*>(a.y) + at;
 #pragma unroll
-                        for (int j = 0; j < W; ++j) o[j] += bias[j];
-                        if (a.res) {
-                            float x[W];
-                            Pack<T>::get(*reinterpret_cast<const uint4*>(static_cast<const T*>(a.res) + at), x);
+                        for (int k = 0; k < L; ++k, y += step) {
+                            const int r = k * W + lane / L;
+                            float o[W];
 #pragma unroll
-                            for (int j = 0; j < W; ++j) o[j] += x[j];
+                            for (int j = 0; j < W; j += 4)
+                                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o[j]), "=f"(o[j + 1]), "=f"(o[j + 2]), "=f"(o[j + 3])
+                                             : "r"(staging + r * 128 + (((lane % L * W + j) / 4 ^ (r & 7)) << 4)) : "memory");
+#pragma unroll
+                            for (int j = 0; j < W; ++j) o[j] += b[j];
+                            if (a.res) {
+                                float x[W];
+                                Pack<T>::get(res[k], x);
+#pragma unroll
+                                for (int j = 0; j < W; ++j) o[j] += x[j];
+                            }
+                            uint4 out = Pack<T>::put(o);
+                            if (a.relu) out = positive(out, T());
+                            if (k * W < most) *reinterpret_cast<uint4*>(y) = out;
                         }
-                        if (a.relu)
-#pragma unroll
-                            for (int j = 0; j < W; ++j) o[j] = fmaxf(o[j], 0.0f);
-                        *reinterpret_cast<uint4*>(static_cast<T*>(a.y) + at) = Pack<T>::put(o);
-                    }
-                } else {      // a row at a time, a lane per channel
-                    const int cl = c0 + lane;
-                    const float bias = a.bias && cl < c1 ? __ldg(a.bias + cl) : 0.0f;
+                    } else {      // a row at a time, a lane per channel
+                        const int cl = c0 + lane;
 #pragma unroll 4
-                    for (int r = 0; r < 32; ++r) {
-                        const int p = ta * 128 + quarter * 32 + r;
-                        float o;
-                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(o) : "r"(staging + r * 128 + ((lane >> 2 ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
-                        if (p < a.a.rows && cl < c1) store_one<T>(a, (size_t)p * a.cout + cl, o, bias);
+                        for (int r = 0; r < 32; ++r) {
+                            float o;
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(o) : "r"(staging + r * 128 + ((lane >> 2 ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
+                            if (r0 + r < a.a.rows && cl < end) store_one<T>(a, (size_t)(r0 + r) * a.cout + cl, o, bias[i]);
+                        }
                     }
                 }
             }
@@ -330,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
         __syncthreads();
         cluster_arrive();
         cluster_wait();
-        const int ta = (int)(first_tile / a.tiles_b), tb = (int)(first_tile % a.tiles_b);
+        const int ta = div_of(first_tile, a.tiles_b), tb = first_tile - ta * a.tiles_b.d;
         const unsigned part = stage0;
         const int total = 128 * n, e0 = (int)((long long)total * rank / a.split), e1 = (int)((long long)total * (rank + 1) / a.split);
 #pragma unroll 1
@@ -361,7 +405,7 @@ struct Shape {
 };
 
 // How a product is cut.
-Shape choose(int rows, int cout, int quads, int sms)
+Shape choose(int rows, int cout, int steps, int sms)
 {
     Shape s = {rows <= 64, 0, 1};
     const int mine = s.swapped ? cout : rows, other = s.swapped ? rows : cout;
@@ -370,7 +414,7 @@ Shape choose(int rows, int cout, int quads, int sms)
     if (other > kMaxN || ta * up_div(other, s.n) < sms)
         while (s.n > 64 && ta * up_div(other, s.n) < sms) s.n = s.n > 192 ? 192 : s.n > 128 ? 128 : 64;
     const long long tiles = ta * up_div(other, s.n);
-    while (s.split < kMaxSplit && tiles * s.split * 2 <= sms && quads >= s.split * 2) s.split *= 2;
+    while (s.split < kMaxSplit && tiles * s.split * 2 <= sms && steps >= s.split * 2) s.split *= 2;
     return s;
 }
 
@@ -414,7 +458,7 @@ ALCS_API int alcs_mx4_product(const void* x, const void* x_scales, int rows, con
     Args a;
     a.blocks = 2 * ((cin + 63) / 64);
     a.quads = (cin + 127) / 128;
-    const Shape s = choose(rows, cout, a.quads, sms);
+    const Shape s = choose(rows, cout, (a.quads + kQuads - 1) / kQuads, sms);
     const Operand ox = {static_cast<const unsigned char*>(x), static_cast<const unsigned char*>(x_scales), rows, (rows + 127) / 128};
     const Operand ow = {static_cast<const unsigned char*>(w), static_cast<const unsigned char*>(w_scales), cout, (cout + 127) / 128};
     a.a = s.swapped ? ow : ox;
@@ -422,12 +466,16 @@ ALCS_API int alcs_mx4_product(const void* x, const void* x_scales, int rows, con
     a.n = s.n;
     a.swapped = s.swapped;
     a.split = s.split;
-    a.tiles_b = (int)up_div(a.b.rows, a.n);
-    a.tiles = (long long)a.a.tiles * a.tiles_b;
-    if (a.tiles > 0x7fffffffll) return ALCS_ERR_SHAPE;
-    a.stage_bytes = 8192 + kStageBlocks * a.n * 16 + 3 * kScaleBytes;
+    const long long tiles_b = up_div(a.b.rows, a.n), tiles = a.a.tiles * tiles_b;
+    if (tiles > 0x7fffffffll) return ALCS_ERR_SHAPE;
+    a.tiles = (int)tiles;
+    a.tiles_b = tc_div((int)tiles_b);
+    // A stage: one or two groups of four blocks, the rows of one tile of a and of one or two of b, and their scales.
+    a.stage_quads = std::min(kQuads, a.quads);
+    a.tile_bytes = std::min(4 * a.stage_quads, a.blocks) * 2048;
+    a.stage_bytes = (a.n > 128 ? 3 : 2) * a.tile_bytes + 3 * a.stage_quads * kScaleBytes;
     constexpr int fixed = kHeader + kEpiWarps * kStaging;
-    a.stages = std::min(kMaxStages, (227 * 1024 - fixed) / a.stage_bytes);
+    a.stages = a.quads ? std::min({kMaxStages, kScaleCols / (12 * a.stage_quads), (227 * 1024 - fixed) / a.stage_bytes}) : 1;
     const size_t part = a.split > 1 ? (size_t)128 * (a.n + 1) * 4 : 0;      // (takes the place of the stages)
     const size_t smem = fixed + std::max((size_t)a.stages * a.stage_bytes, part);
     a.cout = cout;
@@ -436,7 +484,7 @@ ALCS_API int alcs_mx4_product(const void* x, const void* x_scales, int rows, con
     a.bias = bias;
     a.res = residual;
     a.y = y;
-    const int blocks = (int)std::min<long long>(a.tiles * a.split, a.split > 1 ? a.tiles * a.split : sms);
+    const int blocks = a.split > 1 ? a.tiles * a.split : std::min(a.tiles, sms);
     const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     return dt == ALCS_F32 ? launch<float>(a, blocks, smem, dev, st) : dt == ALCS_F16 ? launch<__half>(a, blocks, smem, dev, st)
                                                                                      : launch<__nv_bfloat16>(a, blocks, smem, dev, st);
