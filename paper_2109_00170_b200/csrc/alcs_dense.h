@@ -122,6 +122,30 @@ __device__ __forceinline__ void from_f32(float* p, float v) { *p = v; }
 __device__ __forceinline__ void from_f32(__half* p, float v) { *p = __float2half_rn(v); }
 __device__ __forceinline__ void from_f32(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
+// d = a + b, a - b, a * b, a * b + c on E elements, two per instruction.
+#define ALCS_PAIRS(name, op)                                                                                                                            \
+    template <int E>                                                                                                                                    \
+    __device__ __forceinline__ void name(float (&d)[E], const float (&a)[E], const float (&b)[E])                                                       \
+    {                                                                                                                                                   \
+        if constexpr (E == 1) asm(op ".f32 %0, %1, %2;" : "=f"(d[0]) : "f"(a[0]), "f"(b[0]));                                                           \
+        else                                                                                                                                            \
+            _Pragma("unroll") for (int i = 0; i < E; i += 2)                                                                                            \
+                asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t" op ".f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"            \
+                    : "=f"(d[i]), "=f"(d[i + 1]) : "f"(a[i]), "f"(a[i + 1]), "f"(b[i]), "f"(b[i + 1]));                                                 \
+    }
+ALCS_PAIRS(add, "add.rn")
+ALCS_PAIRS(sub, "sub.rn")
+ALCS_PAIRS(mul, "mul.rn")
+template <int E>
+__device__ __forceinline__ void fma(float (&d)[E], const float (&a)[E], const float (&b)[E], const float (&c)[E])
+{
+    if constexpr (E == 1) d[0] = fmaf(a[0], b[0], c[0]);
+    else
+#pragma unroll
+        for (int i = 0; i < E; i += 2)
+            asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+                : "=f"(d[i]), "=f"(d[i + 1]) : "f"(a[i]), "f"(a[i + 1]), "f"(b[i]), "f"(b[i + 1]), "f"(c[i]), "f"(c[i + 1]));
+}
 // Programmatic dependent launch: the next kernel on the stream may set up, this one waits for what the one before it wrote.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

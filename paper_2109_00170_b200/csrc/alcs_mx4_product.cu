@@ -8,11 +8,12 @@
 // runs; 128 rows x 4 blocks of scales are the 512 bytes that one tcgen05.cp spreads over the four lane quarters.
 //
 // One operand's 128 rows are the rows of a tile (M), `n` rows of the other its columns (N).  Usually pixels are M and output
-// channels N, and a lane of the epilogue has a pixel.  With few pixels the roles are swapped: a tile of 128 channels times 16 pixels
-// costs the tensor cores an eighth of one of 128 pixels.
-// A block of 320 threads: eight warps for the epilogue (two per lane quarter, which take the columns by turns of 32), one that copies, one that
-// multiplies.  Blocks stay and walk over the tiles; the accumulator's 384 columns hold as many tiles as fit, and the epilogue takes a tile into
-// registers before it works on it, so that the next one can start.
+// channels N, and a lane of the epilogue has a pixel.  With few pixels and long rows the roles are swapped (see choose).
+// What bounds it: the copies, first by their number (about 100 cycles each, whatever their size: 2 KB at a time, 16384x4096x4096 took 341 us), now by
+// the way from L2 to the SMs (35 bytes per cycle and SM, 10 TB/s); few columns: the outputs' way to memory.
+// A block has sixteen warps for the epilogue (32 rows x 32 columns of an accumulator each; with eight, 200704x64x256 took 32 us and not 29), one that copies,
+// one that multiplies.  Blocks stay and walk over the tiles.  An accumulator has 128 columns, a tile one or two of the three; the epilogue takes them into
+// registers before it works on them, so that the next tile starts at once.
 // Where the tiles are fewer than SMs and rows are long, a cluster shares a tile: each block multiplies a part of the columns, leaves its
 // partial sums in its shared memory, and adds up, in a fixed order, a share of the outputs over all of them.
 #include <algorithm>
@@ -24,13 +25,13 @@
 namespace alcs {
 namespace {
 
-constexpr int kEpiWarps = 8, kLoadWarp = 8, kMmaWarp = 9;
-constexpr int kThreads = 320;
+constexpr int kEpiWarps = 16, kLoadWarp = 16, kMmaWarp = 17;
+constexpr int kThreads = 576;
 constexpr int kQuads = 2;                               // a stage: up to so many groups of four blocks of 32 columns
 constexpr int kMaxN = 256;
 constexpr int kSlots = 3, kSlotCols = 128;              // tensor memory: accumulators of 128 columns, a tile has one or two; then scales, 12 columns per group
 constexpr int kMaxStages = 8;
-constexpr int kBias = 1024, kHeader = kBias + 8 * 256, kStaging = 32 * 128;      // shared memory: barriers; per epilogue warp: bias, a 32 x 32 piece of the output
+constexpr int kBias = 1024, kHeader = kBias + kEpiWarps * 128, kStaging = 32 * 128;      // shared memory: barriers; per epilogue warp: bias, a 32 x 32 piece of the output
 constexpr int kMaxSplit = 8;
 constexpr int kScaleBytes = 512;
 constexpr int kScaleCols = 512 - kSlots * kSlotCols;
@@ -245,79 +246,52 @@ __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
         }
         __syncwarp();
     } else {
-        const int quarter = warp & 3, half = warp >> 2;
-        const unsigned staging = staging0 + warp * kStaging, bias_at = base + kBias + warp * 256;
+        const int quarter = warp & 3, part_of = warp >> 2;      // the tile's rows, and the columns of an accumulator, that are the warp's: 32 each
+        const unsigned staging = staging0 + warp * kStaging, bias_at = base + kBias + warp * 128;
         constexpr int W = Pack<T>::n, L = 32 / W;      // elements of a store; lanes of a row, and stores of a piece
         unsigned acc = 0, acc_ph = 0;
 #pragma unroll 1
         for (int t = first_tile; t < a.tiles && ok; t += tile_step) {
             const int ta = div_of(t, a.tiles_b), tb = t - ta * a.tiles_b.d;
-            if (a.res && !a.swapped && ta * 128 + quarter * 32 + lane < a.a.rows)      // on its way while the tile is multiplied
+            if (a.res && a.split == 1 && ta * 128 + quarter * 32 + lane < a.a.rows)      // on its way while the tile is multiplied
                 for (int c = tb * n; c < min(tb * n + n, a.cout); c += 128 / (int)sizeof(T))
                     asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const T*>(a.res) + (size_t)(ta * 128 + quarter * 32 + lane) * a.cout + c));
 #pragma unroll 1
             for (unsigned h = 0; h < halves && ok; ++h) {
-                // the warp's pieces of this half: columns 0 and 64 of it (or 32 and 96), 32 each
-                const int piece0 = tb * n + (int)h * kSlotCols + half * 32, end = min(tb * n + n, a.swapped ? a.b.tiles * 128 : a.b.rows);
-                float bias[2] = {0.0f, 0.0f};      // of a lane's column of each
-                if (a.bias && !a.swapped)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (piece0 + 64 * i + lane < end) bias[i] = __ldg(a.bias + piece0 + 64 * i + lane);
-                float v[2][32];
+                const int c0 = tb * n + (int)h * kSlotCols + part_of * 32, end = min(tb * n + n, a.b.rows);
+                const float bias = a.bias && a.split == 1 && c0 + lane < end ? __ldg(a.bias + c0 + lane) : 0.0f;      // of the lane's column
+                float v[32];
                 ok = __all_sync(0xffffffffu, bar_wait(acc_full + 8 * acc, acc_ph));
                 if (!ok) break;
                 tc_after();
-                const unsigned from = tmem + acc * kSlotCols + ((unsigned)quarter << 21) + half * 32;
-                tmem_ld32(from, v[0]);
-                tmem_ld32(from + 64, v[1]);
-                tmem_wait_ld(v[0]);
-                tmem_wait_ld(v[1]);
+                tmem_ld32(tmem + acc * kSlotCols + ((unsigned)quarter << 21) + part_of * 32, v);
+                tmem_wait_ld(v);
                 tc_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(acc_empty + 8 * acc);
                 if (++acc == kSlots) { acc = 0; acc_ph ^= 1u; }
                 if (q0 == q1)      // no columns: nothing was multiplied
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[0][j] = v[1][j] = 0.0f;
+                    for (int j = 0; j < 32; ++j) v[j] = 0.0f;
                 const int row = quarter * 32 + lane;      // of the tile
                 if (a.split > 1) {
                     // partial sums to shared memory, where the stages were: swapped [column][128], else [row][n + 1] (no bank twice)
                     float* const part = reinterpret_cast<float*>(smem + (stage0 - base));
+                    const int col = (int)h * kSlotCols + part_of * 32;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int c0 = (int)h * kSlotCols + half * 32 + 64 * i;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (c0 + j < n) part[a.swapped ? (c0 + j) * 128 + row : row * (n + 1) + c0 + j] = v[i][j];
-                    }
+                    for (int j = 0; j < 32; ++j)
+                        if (col + j < n) part[a.swapped ? (col + j) * 128 + row : row * (n + 1) + col + j] = v[j];
                     continue;
                 }
-                if (a.swapped) {      // a lane has a channel: 32 neighbours of a pixel's row at a time
-                    const int c = ta * 128 + row;
-                    if (c < a.a.rows) {
-                        const float b = a.bias ? __ldg(a.bias + c) : 0.0f;
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) {
-                                const int p = piece0 + 64 * i + j;
-                                if (p < tb * n + n && p < a.b.rows) store_one<T>(a, (size_t)p * a.cout + c, v[i][j], b);
-                            }
-                    }
-                    continue;
-                }
+                if (c0 >= end) continue;
                 // a lane has a pixel: a piece of 32 channels goes through shared memory, so that neighbouring lanes store neighbouring bytes
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int c0 = piece0 + 64 * i;
-                    if (c0 >= end) continue;
+                {
                     __syncwarp();
-                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(bias_at + lane * 4), "f"(bias[i]) : "memory");
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(bias_at + lane * 4), "f"(bias) : "memory");
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(staging + lane * 128 + ((j ^ (lane & 7)) << 4)), "f"(v[i][4 * j]), "f"(v[i][4 * j + 1]),
-                                     "f"(v[i][4 * j + 2]), "f"(v[i][4 * j + 3]) : "memory");
+                        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(staging + lane * 128 + ((j ^ (lane & 7)) << 4)), "f"(v[4 * j]), "f"(v[4 * j + 1]),
+                                     "f"(v[4 * j + 2]), "f"(v[4 * j + 3]) : "memory");
                     __syncwarp();
                     const int r0 = ta * 128 + quarter * 32;      // the piece's first pixel
                     if (a.vec) {
@@ -342,13 +316,11 @@ __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
                             for (int j = 0; j < W; j += 4)
                                 asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o[j]), "=f"(o[j + 1]), "=f"(o[j + 2]), "=f"(o[j + 3])
                                              : "r"(staging + r * 128 + (((lane % L * W + j) / 4 ^ (r & 7)) << 4)) : "memory");
-#pragma unroll
-                            for (int j = 0; j < W; ++j) o[j] += b[j];
+                            add<W>(o, o, b);
                             if (a.res) {
                                 float x[W];
                                 Pack<T>::get(res[k], x);
-#pragma unroll
-                                for (int j = 0; j < W; ++j) o[j] += x[j];
+                                add<W>(o, o, x);
                             }
                             uint4 out = Pack<T>::put(o);
                             if (a.relu) out = positive(out, T());
@@ -360,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
                         for (int r = 0; r < 32; ++r) {
                             float o;
                             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(o) : "r"(staging + r * 128 + ((lane >> 2 ^ (r & 7)) << 4) + (lane & 3) * 4) : "memory");
-                            if (r0 + r < a.a.rows && cl < end) store_one<T>(a, (size_t)(r0 + r) * a.cout + cl, o, bias[i]);
+                            if (r0 + r < a.a.rows && cl < end) store_one<T>(a, (size_t)(r0 + r) * a.cout + cl, o, bias);
                         }
                     }
                 }
@@ -404,17 +376,34 @@ struct Shape {
     int n, split;
 };
 
-// How a product is cut.
+// How a product is cut, `steps` stages long.
+// The width of a tile is that for which the busiest block has least to do, a tile costing its columns and about 64 more (6272x256x1024: 192 columns
+// 9.7 us, 256 11.0; 1568x2048x512: 64 columns 7.7, 256 10.1).
+// A cluster shares a tile, where that gives idle SMs work, if its columns are many: the exchange of partial sums costs 2 to 3 us (256x4096x256: one block per tile
+// 11 us, eight 7.8; 196x512x512: 4.2 and 7).  Then up to 64 pixels are the columns of the tiles, whose partial sums are few (1x2048x512: pixels as columns, eight
+// blocks per tile, 5.7 us; as rows, one block, 7.0; 1x1024x1000: 5.7 and 5.2).  Clusters of eight: no more than find room on the GPU's parts at once
+// (32x2048x2048 in 16 of them: 12.1 us, in clusters of four 7.0).
+int blocks_per_tile(long long tiles, int steps, int sms)
+{
+    for (int split = kMaxSplit; split > 1; split /= 2)
+        if (split <= steps && tiles * split <= (split == 8 ? 96 : sms)) return split;
+    return 1;
+}
 Shape choose(int rows, int cout, int steps, int sms)
 {
-    Shape s = {rows <= 64, 0, 1};
-    const int mine = s.swapped ? cout : rows, other = s.swapped ? rows : cout;
-    const long long ta = up_div(mine, 128);
-    s.n = (int)std::min<long long>(kMaxN, up_div(other, 16) * 16);
-    if (other > kMaxN || ta * up_div(other, s.n) < sms)
-        while (s.n > 64 && ta * up_div(other, s.n) < sms) s.n = s.n > 192 ? 192 : s.n > 128 ? 128 : 64;
-    const long long tiles = ta * up_div(other, s.n);
-    while (s.split < kMaxSplit && tiles * s.split * 2 <= sms && steps >= s.split * 2) s.split *= 2;
+    if (rows <= 64 && steps >= 6) {
+        const int split = blocks_per_tile(up_div(cout, 128), steps, sms);
+        if (split > 1) return {true, (int)up_div(rows, 16) * 16, split};
+    }
+    Shape s = {false, 0, 1};
+    const long long ta = up_div(rows, 128);
+    long long best = 0;
+    for (int n : {256, 192, 128, 64}) {
+        const int width = (int)std::min<long long>(n, up_div(cout, 16) * 16);      // (the only tile's may be any multiple of 16)
+        const long long cost = up_div(ta * up_div(cout, width), sms) * (width + 64);
+        if (!s.n || cost < best) { best = cost; s.n = width; }
+    }
+    if (steps >= 12) s.split = blocks_per_tile(ta * up_div(cout, s.n), steps, sms);
     return s;
 }
 

@@ -147,11 +147,12 @@ class Product:
         assert self.alcs.alcs_dense_status() == 0
 
 
-# rows, cin, cout: single rows; the border of the swapped form; one block, half a step, part of a stage; tiles of 128 rows and their
-# borders; tiles of 64 .. 256 channels; columns shared by clusters of 2, 4, 8; more tiles than SMs; a long sum
+# rows, cin, cout: single rows; one block, half a step, part of a stage; tiles of 128 rows and their borders; tiles of 64 .. 256 channels; columns shared by
+# clusters of 2, 4, 8, with pixels as rows of the tiles and as columns (up to 64); more tiles than SMs; a long sum
 SIZES = [(1, 32, 16), (1, 1, 1), (1, 1024, 1000), (2, 100, 7), (16, 64, 128), (17, 96, 130), (49, 512, 512), (64, 320, 64), (65, 320, 64), (127, 64, 129),
          (128, 128, 128), (129, 160, 257), (300, 1000, 300), (196, 4096, 64), (1955, 100, 150), (700, 96, 1031), (2500, 224, 192), (5000, 64, 200),
-         (9000, 128, 256), (9500, 40, 64), (6000, 130, 520), (33, 8192, 100), (3, 2048, 4096), (40000, 32, 24)]
+         (9000, 128, 256), (9500, 40, 64), (6000, 130, 520), (33, 8192, 100), (3, 2048, 4096), (40000, 32, 24),
+         (1, 1500, 40), (64, 1600, 300), (130, 3500, 70), (250, 3200, 120), (17, 2600, 999)]
 
 
 @pytest.mark.parametrize("rows,cin,cout", SIZES)
@@ -162,7 +163,7 @@ def test_product(alcs, rows, cin, cout, dtype):
     k.check()
 
 
-@pytest.mark.parametrize("rows,cin,cout", [(5, 200, 40), (200, 512, 72), (3000, 128, 72)])
+@pytest.mark.parametrize("rows,cin,cout", [(5, 200, 40), (200, 512, 72), (3000, 128, 72), (5, 2000, 40), (200, 4000, 72)])
 def test_residual_is_the_output_and_odd_starts(alcs, rows, cin, cout):
     torch = _torch()
     k = Product(alcs, rows, cin, cout, "bf16", residual=True, relu=True)
@@ -186,7 +187,7 @@ def test_no_columns(alcs, rows, cout):
     assert (y == bias.clamp(min=0)).all()
 
 
-@pytest.mark.parametrize("rows,cin,cout", [(4, 256, 70), (300, 256, 70)])
+@pytest.mark.parametrize("rows,cin,cout", [(4, 256, 70), (300, 256, 70), (4, 2048, 70), (300, 3200, 70)])
 def test_nan_blocks_take_their_row_and_column_alone(alcs, rows, cin, cout):
     k = Product(alcs, rows, cin, cout, "f32")
     clean = k.run().clone()
