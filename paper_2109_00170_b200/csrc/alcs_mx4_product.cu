@@ -9,8 +9,10 @@
 //
 // One operand's 128 rows are the rows of a tile (M), `n` rows of the other its columns (N).  Usually pixels are M and output
 // channels N, and a lane of the epilogue has a pixel.  With few pixels and long rows the roles are swapped (see choose).
-// What bounds it: the copies, first by their number (about 100 cycles each, whatever their size: 2 KB at a time, 16384x4096x4096 took 341 us), now by
-// the way from L2 to the SMs (35 bytes per cycle and SM, 10 TB/s); few columns: the outputs' way to memory.
+// What bounds it, measured with 16384x4096x4096 (bf16): the number of copies, about 117 cycles each whatever their size (2 KB at a time 341 us, 8 KB 172,
+// 16 KB 129); the instructions of the one thread that issues the tensor cores' (160 us before their descriptors came down to an addition); then both and
+// what is in flight, three stages of 51 KB: 1070 cycles per stage, 512 of them the tensor cores'.  Tiles of 256 x 256 by pairs of blocks (cta_group::2) fetch a
+// third less and were slower, 177 us: the hand-shakes of a stage take longer than it.  Few columns: the outputs' way to memory.
 // A block has sixteen warps for the epilogue (32 rows x 32 columns of an accumulator each; with eight, 200704x64x256 took 32 us and not 29), one that copies,
 // one that multiplies.  Blocks stay and walk over the tiles.  An accumulator has 128 columns, a tile one or two of the three; the epilogue takes them into
 // registers before it works on them, so that the next tile starts at once.
@@ -59,15 +61,18 @@ struct Args {
     void* y;
 };
 
-__device__ __forceinline__ void mma_mx4(unsigned d, unsigned long long a, unsigned long long b, unsigned idesc, unsigned sa, unsigned sb, unsigned acc)
+// The upper half of all matrix descriptors: groups of 8 rows 128 bytes apart, no swizzle.  The lower half: the address, and blocks of 32 columns 2048 bytes
+// apart (K-major: 8 rows x 16 bytes lie together).
+constexpr unsigned kDescHigh = 8u | (1u << 14), kDescLow = 128u << 16;
+__device__ __forceinline__ void mma_mx4(unsigned d, unsigned a, unsigned b, unsigned idesc, unsigned sa, unsigned sb, unsigned acc)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %6, 0;\n\tmov.b64 a, {%1, %7};\n\tmov.b64 b, {%2, %7};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], a, b, %3, [%4], [%5], p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void scales_to_tmem(unsigned d, unsigned long long desc)
+__device__ __forceinline__ void scales_to_tmem(unsigned d, unsigned at)
 {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(d), "l"(desc) : "memory");
+    asm volatile("{\n\t.reg .b64 a;\n\tmov.b64 a, {%1, %2};\n\ttcgen05.cp.cta_group::1.32x128b.warpx4 [%0], a;\n\t}" ::"r"(d), "r"(at), "r"(kDescHigh) : "memory");
 }
 // The address field of a matrix descriptor: 14 bits (in a cluster an address carries the block's rank above them).
 __device__ __forceinline__ unsigned field(unsigned addr) { return addr >> 4 & 0x3fffu; }
@@ -86,6 +91,39 @@ __device__ __forceinline__ float ld_rank(unsigned addr, unsigned rank)      // o
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
     return v;
+}
+
+// E2M1 x E2M1 (type 1 each), scales E8M0; N / 8 is at bit 17, M / 128 at bit 27, which two bytes of the scales at bits 4 and 29.
+constexpr unsigned kIdesc = (1u << 7) | (1u << 10) | (1u << 23);
+constexpr unsigned kSecond = (1u << 5) | (1u << 30);
+
+// A stage's products: scales of `tiles` tiles of rows (0: they are there) to tensor memory, then per 64 columns one or two instructions, whose columns of the
+// accumulators are d0 and d1, rows of shared memory b0 and b1, and scales those of the second operand from column `shift` and column 4 on.  One thread issues all
+// of it, so what counts is how few instructions that takes: the descriptors' lower halves are all that changes.
+template <int PIECES>
+__device__ __forceinline__ void multiply_stage(unsigned a, unsigned b0, unsigned b1, unsigned scales, int Q, int quads, int blocks, unsigned tmem, unsigned shift, int tiles,
+                                               unsigned d0, unsigned d1, unsigned id0, unsigned id1, unsigned add)
+{
+    a = kDescLow | field(a);
+    b0 = kDescLow | field(b0);
+    if (PIECES > 1) b1 = kDescLow | field(b1);
+    scales = kDescLow | field(scales);
+    const int pitch = Q * (kScaleBytes >> 4);
+#pragma unroll
+    for (int g = 0; g < kQuads; ++g) {
+        if (g >= quads || g >= Q) break;
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < tiles) scales_to_tmem(tmem + 12 * g + 4 * i, scales + i * pitch + g * (kScaleBytes >> 4));
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int block = 4 * g + 2 * k;
+            if (block >= blocks) break;
+            const unsigned step = block * 128;
+            mma_mx4(d0, a + step, b0 + step, k ? id0 | kSecond : id0, tmem + 12 * g, tmem + 12 * g + 4 + shift, block > 0 || add);
+            if (PIECES > 1) mma_mx4(d1, a + step, b1 + step, k ? id1 | kSecond : id1, tmem + 12 * g, tmem + 12 * g + 8, block > 0 || add);
+        }
+    }
 }
 
 template <typename T>
@@ -186,16 +224,14 @@ __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
     } else if (warp == kMmaWarp) {
         if (elect_one()) {
             unsigned stage = 0, ph = 0, acc = 0, acc_ph = 1;      // (a slot's phase turns when the ring has)
-            // E2M1 x E2M1 (type 1 each), scales E8M0; N / 8 at bit 17, M / 128 at bit 27
-            const unsigned idesc = (1u << 7) | (1u << 10) | (1u << 23) | (1u << 27);
-            // K-major, no swizzle: blocks of 32 columns 2048 bytes apart, groups of 8 rows 128 bytes
-            const unsigned long long dm = (128ull << 16) | (8ull << 32) | (1ull << 46), ds = (8ull << 16) | (8ull << 32) | (1ull << 46);
 #pragma unroll 1
             for (int t = first_tile; t < a.tiles && ok; t += tile_step) {
                 const int tb = t - div_of(t, a.tiles_b) * a.tiles_b.d;
                 // the columns that are rows of b's first tile, and of its second
-                const unsigned off = (unsigned)(tb * n & 127), n0 = min((unsigned)n, 128 - off), n1 = n - n0;
+                const unsigned off = (unsigned)(tb * n & 127), n0 = min((unsigned)n, 128 - off);
                 const int nt = (min(tb * n + n, a.b.tiles * 128) - 1 >> 7) - (tb * n >> 7) + 1;
+                const unsigned n1 = nt > 1 ? n - n0 : 0;
+                const unsigned id0 = kIdesc | (1u << 27) | (n0 >> 3) << 17, id1 = kIdesc | (1u << 27) | (n1 >> 3) << 17;
                 unsigned d[2], bar[2];
                 for (unsigned h = 0; h < halves; ++h) {
                     d[h] = tmem + acc * kSlotCols;
@@ -208,29 +244,19 @@ __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
                     ok = bar_wait(full + 8 * stage, ph);
                     if (!ok) break;
                     tc_after();
-                    const unsigned at = stage0 + stage * a.stage_bytes, to_s = at + a.stage_bytes - 3 * Q * kScaleBytes;
-                    const int nq = min(Q, a.quads - q * Q);
-#pragma unroll 1
-                    for (int g = 0; g < nq; ++g) {
-                        const unsigned sa = tmem + kSlots * kSlotCols + 12 * (stage * Q + g), sb = sa + 4;
-                        for (int i = 0; i <= nt; ++i) scales_to_tmem(sa + 4 * i, ds | field(to_s + (i * Q + g) * kScaleBytes));
-                        const int steps = min(4, a.blocks - (q * Q + g) * 4) / 2;
-#pragma unroll 1
-                        for (int k = 0; k < steps; ++k) {      // two blocks each; bits 4 and 29: which bytes of the scales
-                            const unsigned id = idesc | (unsigned)k << 5 | (unsigned)k << 30, acc_in = q > q0 || g > 0 || k > 0;
-                            const unsigned col = at + (g * 4 + k * 2) * 2048;
-                            const unsigned first = at + a.tile_bytes + (g * 4 + k * 2) * 2048 + off * 16;
-                            const unsigned m0 = min(n0, 128u), m1 = n - m0;      // columns of the two accumulators
-                            // (a tile that starts in the middle of 128 rows: its accumulators' border is not that of the tiles of rows)
-                            if (off == 0 || n1 == 0 || nt == 1) {
-                                mma_mx4(d[0], dm | field(col), dm | field(first), id | (m0 >> 3) << 17, sa, sb + (off >> 5), acc_in);
-                                if (m1 && nt > 1) mma_mx4(d[1], dm | field(col), dm | field(first - off * 16 + a.tile_bytes), id | (m1 >> 3) << 17, sa, sb + 4, acc_in);
-                            } else {      // 64 rows of the first, 64 and 64 of the second
-                                mma_mx4(d[0], dm | field(col), dm | field(first), id | 8u << 17, sa, sb + 2, acc_in);
-                                mma_mx4(d[0] + 64, dm | field(col), dm | field(first - off * 16 + a.tile_bytes), id | 8u << 17, sa, sb + 4, acc_in);
-                                mma_mx4(d[1], dm | field(col), dm | field(first - off * 16 + a.tile_bytes + 64 * 16), id | 8u << 17, sa, sb + 6, acc_in);
-                            }
-                        }
+                    const unsigned at = stage0 + stage * a.stage_bytes, b0 = at + a.tile_bytes + off * 16, to_s = at + a.stage_bytes - 3 * Q * kScaleBytes;
+                    const unsigned to = tmem + kSlots * kSlotCols + 12 * stage * Q;
+                    const int nq = a.quads - q * Q, nb = a.blocks - q * 4 * Q;
+                    if (n1 == 0) {
+                        multiply_stage<1>(at, b0, 0, to_s, Q, nq, nb, to, off >> 5, 2, d[0], 0, id0, 0, q > q0);
+                    } else if (off == 0) {
+                        multiply_stage<2>(at, b0, b0 + a.tile_bytes, to_s, Q, nq, nb, to, 0, 3, d[0], d[1], id0, id1, q > q0);
+                    } else {
+                        // A tile that starts in the middle of 128 rows: its accumulators' border is not that of the tiles of rows.  64 rows of the first, 64 and 64 of
+                        // the second; the scales are there from the first call on.
+                        const unsigned id = kIdesc | (1u << 27) | 8u << 17, b1 = at + 2 * a.tile_bytes;
+                        multiply_stage<2>(at, b0, b1, to_s, Q, nq, nb, to, 2, 3, d[0], d[0] + 64, id, id, q > q0);
+                        multiply_stage<1>(at, b1 + 64 * 16, 0, to_s, Q, nq, nb, to, 6, 0, d[1], 0, id, 0, q > q0);
                     }
                     mma_commit(empty + 8 * stage);
                     if (++stage == (unsigned)S) { stage = 0; ph ^= 1u; }

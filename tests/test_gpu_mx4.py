@@ -152,7 +152,8 @@ class Product:
 SIZES = [(1, 32, 16), (1, 1, 1), (1, 1024, 1000), (2, 100, 7), (16, 64, 128), (17, 96, 130), (49, 512, 512), (64, 320, 64), (65, 320, 64), (127, 64, 129),
          (128, 128, 128), (129, 160, 257), (300, 1000, 300), (196, 4096, 64), (1955, 100, 150), (700, 96, 1031), (2500, 224, 192), (5000, 64, 200),
          (9000, 128, 256), (9500, 40, 64), (6000, 130, 520), (33, 8192, 100), (3, 2048, 4096), (40000, 32, 24),
-         (1, 1500, 40), (64, 1600, 300), (130, 3500, 70), (250, 3200, 120), (17, 2600, 999)]
+         (1, 1500, 40), (64, 1600, 300), (130, 3500, 70), (250, 3200, 120), (17, 2600, 999),
+         (4900, 800, 2200), (6400, 1025, 2304), (2600, 2100, 4100)]
 
 
 @pytest.mark.parametrize("rows,cin,cout", SIZES)
