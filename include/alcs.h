@@ -457,8 +457,8 @@ ALCS_API int alcs_spconv2d_plan(const alcs_packed* w, int n, int cin, int h, int
  *     z = gamma[channel] * xh + beta[channel],  y = act(z),  act the identity, ALCS_RELU or ALCS_SILU (flags).
  * x and y are device [n][h*wd][c] (NHWC), contiguous, of type dt, aligned to their element size; y may be x itself, but not
  * overlap it otherwise.  gamma and beta are device fp32 [c] or NULL (1 and 0); mean and rstd receive mu and rstd, device fp32
- * [n][groups], or are NULL.  Statistics and everything up to the rounding of y are fp32; the variance is that of values with
- * their mean (of the part of the group a thread block has) taken off, so that a mean far from 0 costs no accuracy.  An infinity
+ * [n][groups], or are NULL.  Statistics and everything up to the rounding of y are fp32; squares are summed
+ * of values less one of a few dozen neighbours, and of differences of means, so that a mean far from 0 costs no accuracy.  An infinity
  * or NaN makes its group of its image NaN.  ReLU turns NaN into 0, as in the convolutions.
  *
  * alcs_group_norm_backward: for the derivative dy of a loss by y, with dz = dy * act'(z) (act' of ReLU at 0 is 0) and t = gamma * dz,
@@ -475,8 +475,7 @@ ALCS_API int alcs_spconv2d_plan(const alcs_packed* w, int n, int cin, int h, int
  * h*wd == 0 is a successful no-op, but for dgamma and dbeta, which become 0.
  * Errors: INVALID_ARG (null, misaligned or overlapping buffers, host memory, negative sizes, groups < 1, an eps that is negative or not finite, both
  * activations, workspace too small), SHAPE (c not a multiple of groups, h*wd or n*c of 2^30 and more, c above 65536),
- * UNSUPPORTED (more than 8192 channels per group),
- * STATE (memory of another device), CUDA.
+ * UNSUPPORTED (more than 8192 channels per group), STATE (memory of another device), CUDA.
  * ------------------------------------------------------------------------------------------- */
 ALCS_API size_t alcs_group_norm_workspace(int n, int h, int wd, int c, int groups, alcs_dtype dt);
 ALCS_API int alcs_group_norm(const void* x, void* y, int n, int h, int wd, int c, int groups, const float* gamma, const float* beta,
@@ -524,11 +523,10 @@ ALCS_API int alcs_mx4_dequantize(const void* data, const void* scales, int rows,
 ALCS_API int alcs_mx4_product(const void* x, const void* x_scales, int rows, const void* w, const void* w_scales, int cout, int cin,
                               void* y, const float* bias, const void* residual, unsigned flags, alcs_dtype dt, void* cuda_stream);
 /*
- * alcs_dense_status: the error word of the current device's alcs_group_norm, alcs_group_norm_backward and alcs_mx4_product calls
- * (synchronises with the device).  *code is 0 unless a kernel gave up one of its bounded waits: 1 = for data, 2 = for a free pipeline stage; the
+ * alcs_mx4_status: the error word of the current device's alcs_mx4_product calls (synchronises with the device).  *code is 0 unless a kernel gave up one of its bounded waits: 1 = for data, 2 = for a free pipeline stage; the
  * outputs of that launch are then incomplete.
  */
-ALCS_API int alcs_dense_status(int* code);
+ALCS_API int alcs_mx4_status(int* code);
 
 /* ---------------------------------------------------------------------------------------------
  * Latency model and projection with bisection.

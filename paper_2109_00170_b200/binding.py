@@ -30,7 +30,7 @@ EXPORTS = ["alcs_strerror", "alcs_last_cuda_error", "alcs_version", "alcs_pack",
            "alcs_spconv1x1", "alcs_spconv1x1_cfg", "alcs_spconv1x1_ex",
            "alcs_spconv1x1_plan", "alcs_spconv1x1_tune", "alcs_spconv1x1_set_cfg", "alcs_spconv1x1_host_workspace",
            "alcs_spconv1x1_host", "alcs_spconv1x1_noalloc", "alcs_spconv2d", "alcs_spconv2d_cfg", "alcs_spconv2d_plan", "alcs_group_norm_workspace", "alcs_group_norm",
-           "alcs_group_norm_backward", "alcs_mx4_bytes", "alcs_mx4_quantize", "alcs_mx4_dequantize", "alcs_mx4_product", "alcs_dense_status", "alcs_layer_latency", "alcs_network_latency",
+           "alcs_group_norm_backward", "alcs_mx4_bytes", "alcs_mx4_quantize", "alcs_mx4_dequantize", "alcs_mx4_product", "alcs_mx4_status", "alcs_layer_latency", "alcs_network_latency",
            "alcs_project_bisection", "alcs_probe_fma_peak", "alcs_probe_lds", "alcs_probe_segment_loop",
            "alcs_stack_create", "alcs_stack_run", "alcs_stack_destroy", "alcs_stack_tune", "alcs_stack_layer_cfg"]
 
@@ -150,7 +150,7 @@ def lib():
     L.alcs_mx4_quantize.argtypes = [vp, i, i, ll, i, vp, vp, vp]
     L.alcs_mx4_dequantize.argtypes = [vp, vp, i, i, vp, ll, i, vp]
     L.alcs_mx4_product.argtypes = [vp, vp, i, vp, vp, i, i, vp, vp, vp, u, i, vp]
-    L.alcs_dense_status.argtypes = [ip]
+    L.alcs_mx4_status.argtypes = [ip]
     L.alcs_layer_latency.argtypes = [C.POINTER(LatencyTable), C.c_int64, C.POINTER(C.c_double)]
     L.alcs_network_latency.argtypes = [C.c_double, C.POINTER(LatencyTable), i, C.POINTER(C.c_int64), C.POINTER(C.c_double)]
     L.alcs_project_bisection.argtypes = [C.POINTER(vp), ip, ip, i, i, C.POINTER(LatencyTable), C.c_double, C.c_double,
@@ -497,10 +497,10 @@ def alcs_mx4_product(x, x_scales, rows: int, w, w_scales, cout: int, cin: int, y
         _check(st, "alcs_mx4_product")
 
 
-def alcs_dense_status() -> int:
-    """Error word of the current device's group norms and 4-bit products: 0 unless a kernel gave up a bounded wait."""
+def alcs_mx4_status() -> int:
+    """Error word of the current device's 4-bit products: 0 unless a kernel gave up a bounded wait."""
     code = C.c_int(0)
-    _check(lib().alcs_dense_status(code), "alcs_dense_status")
+    _check(lib().alcs_mx4_status(code), "alcs_mx4_status")
     return code.value
 
 

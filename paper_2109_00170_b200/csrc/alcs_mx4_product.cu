@@ -30,7 +30,6 @@ namespace {
 constexpr int kEpiWarps = 16, kLoadWarp = 16, kMmaWarp = 17;
 constexpr int kThreads = 576;
 constexpr int kQuads = 2;                               // a stage: up to so many groups of four blocks of 32 columns
-constexpr int kMaxN = 256;
 constexpr int kSlots = 3, kSlotCols = 128;              // tensor memory: accumulators of 128 columns, a tile has one or two; then scales, 12 columns per group
 constexpr int kMaxStages = 8;
 constexpr int kBias = 1024, kHeader = kBias + kEpiWarps * 128, kStaging = 32 * 128;      // shared memory: barriers; per epilogue warp: bias, a 32 x 32 piece of the output
@@ -38,7 +37,7 @@ constexpr int kMaxSplit = 8;
 constexpr int kScaleBytes = 512;
 constexpr int kScaleCols = 512 - kSlots * kSlotCols;
 
-__device__ int g_error;      // see alcs_dense_status
+__device__ int g_error;      // see alcs_mx4_status
 
 struct Operand {
     const unsigned char *data, *scales;
@@ -505,10 +504,11 @@ ALCS_API int alcs_mx4_product(const void* x, const void* x_scales, int rows, con
                                                                                      : launch<__nv_bfloat16>(a, blocks, smem, dev, st);
 }
 
-ALCS_API int alcs_dense_status(int* code)
+ALCS_API int alcs_mx4_status(int* code)
 {
     using namespace alcs;
     if (!code) return ALCS_ERR_INVALID_ARG;
+    ALCS_CUDA(cudaDeviceSynchronize());
     ALCS_CUDA(cudaMemcpyFromSymbol(code, g_error, sizeof(int)));
     return ALCS_OK;
 }

@@ -74,6 +74,11 @@ __device__ __forceinline__ void get(const raw_t<T, E>& r, float (&v)[E])
         v[0] = to_f32(t);
     } else if constexpr (E * sizeof(T) == 16) {
         Pack<T>::get(r, v);
+    } else if constexpr (sizeof(T) == 4) {
+        v[0] = __uint_as_float(r.x);
+        v[1] = __uint_as_float(r.y);
+    } else if constexpr (E == 2) {
+        unpack2(r, v, T());
     } else {
         unpack2(r.x, v, T());
         unpack2(r.y, v + 2, T());
@@ -84,6 +89,8 @@ __device__ __forceinline__ void store(T* p, const float (&v)[E])
 {
     if constexpr (E == 1) from_f32(p, v[0]);
     else if constexpr (E * sizeof(T) == 16) *reinterpret_cast<uint4*>(p) = Pack<T>::put(v);
+    else if constexpr (sizeof(T) == 4) *reinterpret_cast<uint2*>(p) = make_uint2(__float_as_uint(v[0]), __float_as_uint(v[1]));
+    else if constexpr (E == 2) *reinterpret_cast<unsigned*>(p) = pack2(v[0], v[1], T());
     else *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v[0], v[1], T()), pack2(v[2], v[3], T()));
 }
 
@@ -97,8 +104,12 @@ __device__ __forceinline__ void set(float (&d)[E], float v)
 template <int E>
 __device__ __forceinline__ void load_shared(float (&d)[E], const float* p)
 {
-    if constexpr (E == 1) d[0] = p[0];
-    else
+    if constexpr (E == 1) {
+        d[0] = p[0];
+    } else if constexpr (E == 2) {
+        const float2 f = *reinterpret_cast<const float2*>(p);
+        d[0] = f.x; d[1] = f.y;
+    } else
 #pragma unroll
         for (int j = 0; j < E; j += 4) {
             const float4 f = *reinterpret_cast<const float4*>(p + j);
@@ -109,6 +120,7 @@ template <int E>
 __device__ __forceinline__ void store_shared(float* p, const float (&d)[E])
 {
     if constexpr (E == 1) p[0] = d[0];
+    else if constexpr (E == 2) *reinterpret_cast<float2*>(p) = make_float2(d[0], d[1]);
     else
 #pragma unroll
         for (int j = 0; j < E; j += 4) *reinterpret_cast<float4*>(p + j) = make_float4(d[j], d[j + 1], d[j + 2], d[j + 3]);
@@ -197,6 +209,7 @@ __device__ __forceinline__ void put_dz(raw_t<T, E>* a, raw_t<T, E>* b, const flo
 {
     if constexpr (sizeof(T) == 4) {
         if constexpr (E == 1) *a = __float_as_uint(d[0]);
+        else if constexpr (E == 2) *a = make_uint2(__float_as_uint(d[0]), __float_as_uint(d[1]));
         else *a = Pack<float>::put(d);
     } else if constexpr (E == 8) {
         *a = Pack<float>::put(d);
@@ -204,6 +217,9 @@ __device__ __forceinline__ void put_dz(raw_t<T, E>* a, raw_t<T, E>* b, const flo
     } else if constexpr (E == 4) {
         *a = make_uint2(__float_as_uint(d[0]), __float_as_uint(d[1]));
         *b = make_uint2(__float_as_uint(d[2]), __float_as_uint(d[3]));
+    } else if constexpr (E == 2) {
+        *a = __float_as_uint(d[0]);
+        *b = __float_as_uint(d[1]);
     } else {
         *a = (unsigned short)(__float_as_uint(d[0]) & 0xffffu);
         *b = (unsigned short)(__float_as_uint(d[0]) >> 16);
@@ -214,6 +230,7 @@ __device__ __forceinline__ void get_dz(const raw_t<T, E>* a, const raw_t<T, E>* 
 {
     if constexpr (sizeof(T) == 4) {
         if constexpr (E == 1) d[0] = __uint_as_float(*a);
+        else if constexpr (E == 2) get<T, E>(*a, d);
         else Pack<float>::get(*a, d);
     } else if constexpr (E == 8) {
         Pack<float>::get(*a, d);
@@ -221,6 +238,9 @@ __device__ __forceinline__ void get_dz(const raw_t<T, E>* a, const raw_t<T, E>* 
     } else if constexpr (E == 4) {
         const uint2 x = *a, y = *b;
         d[0] = __uint_as_float(x.x); d[1] = __uint_as_float(x.y); d[2] = __uint_as_float(y.x); d[3] = __uint_as_float(y.y);
+    } else if constexpr (E == 2) {
+        d[0] = __uint_as_float(*a);
+        d[1] = __uint_as_float(*b);
     } else {
         d[0] = __uint_as_float((unsigned)*a | (unsigned)*b << 16);
     }
@@ -990,13 +1010,14 @@ NormPlan make_plan(int n, int hw, int c, int groups, int elt, int align, bool ba
 {
     NormPlan p = {};
     const int cg = c / groups;
-    p.e = c * elt % 16 == 0 && align % 16 == 0 ? 16 / elt : elt == 2 && c % 4 == 0 && align % 8 == 0 ? 4 : 1;
+    for (p.e = 16 / elt; p.e > 1 && (c % p.e || align % (p.e * elt)); p.e /= 2) {}      // elements of a load
     int gs0 = p.e / gcd(p.e, cg);                       // groups whose channels are whole loads
-    // One pass, by what was measured to matter: how much of a sector a span's pixels are, how many blocks of an SM can be in different phases,
-    // how much of a block's time its sums take, how many SMs have work.
+    // One pass: the spans and clusters of the smallest estimate, in microseconds.  A block's loads and sums take an SM's issue slots (the more blocks are there,
+    // the better they are filled), but no less than their latencies; memory is idle meanwhile as far as all blocks are at the same; spans that are parts of
+    // sectors cost memory time.  Fitted to sweeps of six shapes, from 4x14x14x512 (8 to 12 us) to 32x112x112x64 (55 to 75): within 15 % of the best of each.
     double best = 0;
     // The backward pass holds x, dy and, with SiLU, dz: few blocks per SM.  Large calls, which keep the memory busy either way, are faster in two passes
-    // (64 images of 56x56x256, SiLU: 162 us in one pass, 110 in two; 32 of 28x28x256: 21 and 25).
+    // (64 images of 56x56x256, SiLU: 162 us in one pass, 106 in two; 32 of 28x28x256: 18 and 25).
     for (int gs = gs0; !back || (long long)n * hw * c * elt <= (32 << 20); gs *= 2) {
         const long long nv = (long long)gs * cg / p.e, nch = up_div((long long)gs * cg, 4) * 4;
         if (gs > kMaxSpanGroups || gs > std::max(gs0, groups) || nv > kThreads) break;
@@ -1008,14 +1029,14 @@ NormPlan make_plan(int n, int hw, int c, int groups, int elt, int align, bool ba
             const size_t smem = (size_t)kThreads * p.e * 8 + (back ? 6 : 3) * nch * 4 + (size_t)loads * slots * kThreads * p.e * elt;
             if (smem > 200 * 1024) continue;
             const int resident = std::min<int>(back ? 6 : 8, (int)(225 * 1024 / (smem + 1024)));
-            const double blocks = (double)n * up_div(groups, gs) * cluster;
-            const double sector = bytes >= 128 ? 1 : bytes >= 64 ? 0.95 : bytes >= 32 ? 0.8 : 0.5;
-            const double overlap = resident >= 4 ? 1 : resident == 3 ? 0.95 : resident == 2 ? 0.8 : 0.55;
-            const double busy = std::min(1.0, blocks / sms), waves = blocks / (sms * resident);
-            const double tail = waves > 1 ? waves / std::ceil(waves) : 1;
-            const double score = sector * overlap * busy * tail * loads / (loads + (cluster > 8 ? 5.0 : cluster > 1 ? 4.0 : 3.0));
-            if (score > best) {
-                best = score;
+            const double per_sm = (double)n * up_div(groups, gs) * cluster / sms, at_once = std::min((double)resident, std::max(1.0, per_sm));
+            const double per_load = 0.015 + p.e * (back ? (silu ? 0.017 : 0.010) : silu ? 0.0085 : 0.0065);
+            const double latency = 2.5 + 0.1 * loads + (cluster > 1 ? 1.5 : 0) + (cluster > 8 ? 1.5 : 0);
+            const double slots_time = per_sm * (1 + loads * per_load) * (at_once >= 6 ? 1 : at_once >= 4 ? 1.15 : 1.4);
+            const double memory = (double)n * hw * c * elt * (back ? 3 : 2) / 6.2e6 * (bytes >= 64 ? 1 : bytes >= 32 ? 1.25 : 2) * (per_sm > 2 * at_once ? 0.6 : 1);
+            const double us = std::max(slots_time, std::ceil(per_sm / at_once) * latency) + memory;
+            if (best == 0 || us < best) {
+                best = us;
                 p.gs = gs; p.cluster = p.chunks = cluster; p.chunk = chunk; p.loads = loads; p.smem = smem;
             }
         }
@@ -1070,6 +1091,7 @@ template <typename T>
 Kernel kernel_of(int e, bool back, int which, bool silu)
 {
     if (e == 1) return kernel_of<T, 1>(back, which, silu);
+    if (e == 2) return kernel_of<T, 2>(back, which, silu);
     if constexpr (sizeof(T) == 2) {
         if (e == 4) return kernel_of<T, 4>(back, which, silu);
         return kernel_of<T, 8>(back, which, silu);
@@ -1143,7 +1165,7 @@ ALCS_API size_t alcs_group_norm_workspace(int n, int h, int wd, int c, int group
     if (!known_type(dt) || check_shape(n, h, wd, c, groups) || n == 0 || c == 0 || (long long)h * wd == 0) return 0;
     size_t most = 0;
     // (whatever the alignment of the buffers and the activation)
-    for (int align : {16, 8, 4})
+    for (int align : {16, 8, 4, 2})
         for (bool back : {false, true})
             for (bool silu : {false, true}) {
                 const NormPlan p = make_plan(n, h * wd, c, groups, (int)elt_bytes(dt), align, back, silu, 148);

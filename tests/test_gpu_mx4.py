@@ -144,7 +144,7 @@ class Product:
         got = f64(self.y)
         assert np.isfinite(got).all()
         assert (np.abs(got - ref) <= bound).all(), float((np.abs(got - ref) / bound).max())
-        assert self.alcs.alcs_dense_status() == 0
+        assert self.alcs.alcs_mx4_status() == 0
 
 
 # rows, cin, cout: single rows; one block, half a step, part of a stage; tiles of 128 rows and their borders; tiles of 64 .. 256 channels; columns shared by
@@ -242,7 +242,7 @@ def test_streams_graphs_and_the_same_bits(alcs):
         torch.cuda.synchronize()
         for k, w in zip(work, want):
             assert (k.y == w).all()
-    assert alcs.alcs_dense_status() == 0
+    assert alcs.alcs_mx4_status() == 0
 
 
 def test_outputs_and_inputs_beyond_32_bits(alcs):
