@@ -7,6 +7,7 @@
 #include <algorithm>
 
 #include "alcs_dense.h"
+#include "alcs_tc.h"
 
 namespace alcs {
 namespace {
@@ -18,44 +19,84 @@ struct Args {
     void* y;
     unsigned char *data, *scales;
     long long ld;
-    int rows, cols, blocks, quads;      // blocks of a row as stored (even), groups of four
+    int rows, cols, blocks;             // blocks of a row as stored (even)
+    TcDiv quads;                        // groups of four
     long long units;                    // 8 rows x 4 blocks
 };
 
-// Two values as a byte of two codes, the first in the low half.
-__device__ __forceinline__ unsigned encode4(const float* v)      // four values, 16 bits
+// u / quads: a multiplication where u has 31 bits
+__device__ __forceinline__ int band_of(const Args& a, long long u)
+{
+    if (a.units < 0x7fffffffll) return (int)((unsigned long long)(unsigned)u * a.quads.mul >> a.quads.shift);
+    return (int)(u / a.quads.d);
+}
+
+// Eight values as codes, the first in the lowest four bits.
+__device__ __forceinline__ unsigned encode8(const float* v)
 {
     unsigned r;
-    asm("{\n\t.reg .b8 a, b, z;\n\tcvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
-        "mov.b32 %0, {a, b, a, b};\n\t}" : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]));
-    return r & 0xffffu;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tcvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\tmov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return r;
 }
 
-// Values of four codes (16 bits).
-__device__ __forceinline__ void decode4(unsigned r, float* v)
+// Values of eight codes.
+__device__ __forceinline__ void decode8(unsigned r, float* v)
 {
-    unsigned lo, hi;
-    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %2;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t}"
-        : "=r"(lo), "=r"(hi) : "r"(r));
-    unpack2(lo, v, __half());
-    unpack2(hi, v + 2, __half());
+    unsigned h[4];
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}" : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(r));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(h[i], v + 2 * i, __half());
 }
 
-// A lane's 8 values of a row, from column c on; zeros behind the last column.
+// A lane's 8 values of a row as they lie in memory, from column c on; zeros behind the last column.
+template <typename T> struct Eight { uint4 r[8 * sizeof(T) / 16]; };
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T* row, int c, int cols, float (&v)[8])
+__device__ __forceinline__ void load8(const T* row, int c, int cols, Eight<T>& v)
 {
+    constexpr int n = Pack<T>::n;
     if (VEC) {      // (cols is a multiple of 16 bytes' elements)
 #pragma unroll
-        for (int i = 0; i < 8; i += Pack<T>::n) {
-            uint4 r = make_uint4(0, 0, 0, 0);
-            if (c + i < cols) asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(row + c + i));
-            Pack<T>::get(r, v + i);
+        for (int i = 0; i < 8 / n; ++i) {
+            v.r[i] = make_uint4(0, 0, 0, 0);
+            if (c + i * n < cols)
+                asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.r[i].x), "=r"(v.r[i].y), "=r"(v.r[i].z), "=r"(v.r[i].w) : "l"(row + c + i * n));
         }
     } else {
+        T* const e = reinterpret_cast<T*>(&v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? to_f32(row[c + i]) : 0.0f;
+        for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? row[c + i] : T(0.0f);
     }
+}
+
+__device__ __forceinline__ unsigned max_halves(unsigned a, unsigned b)      // of 16 bits each
+{
+    unsigned r;
+    asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// The largest magnitude of a block, of which four lanes have 8 values each, as fp32 bits: as integers magnitudes have the numbers' order, NaN above infinity.  16-bit
+// types are compared two at a time, as they are.
+__device__ __forceinline__ unsigned largest(const Eight<float>& v)
+{
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) top = max(max(top, max(v.r[i].x & 0x7fffffffu, v.r[i].y & 0x7fffffffu)), max(v.r[i].z & 0x7fffffffu, v.r[i].w & 0x7fffffffu));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    return max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+}
+template <typename T>
+__device__ __forceinline__ unsigned largest(const Eight<T>& v)
+{
+    const uint4& r = v.r[0];
+    unsigned top = max_halves(max_halves(r.x & 0x7fff7fffu, r.y & 0x7fff7fffu), max_halves(r.z & 0x7fff7fffu, r.w & 0x7fff7fffu));
+    top = max_halves(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max_halves(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    float f[2];
+    unpack2(max(top & 0xffffu, top >> 16), f, T());
+    return __float_as_uint(f[0]) & 0x7fffffffu;
 }
 
 template <typename T, bool VEC>
@@ -67,33 +108,32 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const Args a)
     const long long warps = (long long)gridDim.x * (kThreads / 32);
 #pragma unroll 1
     for (long long u = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); u < a.units; u += warps) {
-        const int quad = (int)(u % a.quads), r = (int)(u / a.quads) * 8 + (lane >> 2);
+        const int band = band_of(a, u), quad = (int)(u - (long long)band * a.quads.d), r = band * 8 + (lane >> 2);
         const bool mine = r < a.rows;
         const T* row = static_cast<const T*>(a.x) + (size_t)r * a.ld;
-        float v[4][8];
+        Eight<T> v[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) load8<T, VEC>(row, (quad * 4 + b) * 32 + q * 8, mine ? a.cols : 0, v[b]);
         unsigned char* to = a.data + ((size_t)(r >> 7) * a.blocks + quad * 4) * 2048 + (r & 127) * 16 + q * 4;
         unsigned scales = 0;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            unsigned top = 0;      // of magnitudes, as integers: their order is that of the numbers, NaN above infinity
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[b][i]) & 0x7fffffffu);
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const int e = (int)(top >> 23);             // floor(log2) + 127; 0 for subnormal numbers, whose scale is 2^-127, too
+            const int e = (int)(largest(v[b]) >> 23);   // floor(log2) + 127; 0 for subnormal numbers, whose scale is 2^-127, too
             const bool finite = e < 255;
             const int s = finite ? max(e - 2, 0) : 255;
             const float inv = __uint_as_float((unsigned)(254 - (finite ? s : 127)) << 23);      // 2^(127 - s)
+            float f[8], k[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[b][i] = finite ? v[b][i] * inv : 0.0f;
+            for (int i = 0; i < 8; i += Pack<T>::n) Pack<T>::get(v[b].r[i / Pack<T>::n], f + i);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) k[i] = inv;
+            mul<8>(f, f, k);
             scales |= (unsigned)s << (8 * b);
-            const unsigned code = encode4(v[b]) | encode4(v[b] + 4) << 16;
+            const unsigned code = finite ? encode8(f) : 0u;
             if (mine && quad * 4 + b < a.blocks) *reinterpret_cast<unsigned*>(to + b * 2048) = code;
         }
         if (mine && q == 0)
-            *reinterpret_cast<unsigned*>(a.scales + ((size_t)(r >> 7) * a.quads + quad) * 512 + (r & 31) * 16 + (r >> 5 & 3) * 4) = scales;
+            *reinterpret_cast<unsigned*>(a.scales + ((size_t)(r >> 7) * a.quads.d + quad) * 512 + (r & 31) * 16 + (r >> 5 & 3) * 4) = scales;
     }
 }
 
@@ -106,10 +146,10 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const Args a)
     const long long warps = (long long)gridDim.x * (kThreads / 32);
 #pragma unroll 1
     for (long long u = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5); u < a.units; u += warps) {
-        const int quad = (int)(u % a.quads), r = (int)(u / a.quads) * 8 + (lane >> 2);
+        const int band = band_of(a, u), quad = (int)(u - (long long)band * a.quads.d), r = band * 8 + (lane >> 2);
         if (r >= a.rows) continue;
         const unsigned char* from = a.data + ((size_t)(r >> 7) * a.blocks + quad * 4) * 2048 + (r & 127) * 16 + q * 4;
-        const unsigned scales = __ldg(reinterpret_cast<const unsigned*>(a.scales + ((size_t)(r >> 7) * a.quads + quad) * 512 + (r & 31) * 16 + (r >> 5 & 3) * 4));
+        const unsigned scales = __ldg(reinterpret_cast<const unsigned*>(a.scales + ((size_t)(r >> 7) * a.quads.d + quad) * 512 + (r & 31) * 16 + (r >> 5 & 3) * 4));
         unsigned code[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) code[b] = quad * 4 + b < a.blocks ? __ldg(reinterpret_cast<const unsigned*>(from + b * 2048)) : 0u;
@@ -119,11 +159,11 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const Args a)
             const unsigned s = scales >> (8 * b) & 255u;
             // 2^(s - 127): a subnormal number for s = 0; 255 is the exponent of NaN
             const float scale = __uint_as_float(s == 0 ? 0x00400000u : s == 255 ? 0x7fffffffu : s << 23);
-            float v[8];
-            decode4(code[b], v);
-            decode4(code[b] >> 16, v + 4);
+            float v[8], k[8];
+            decode8(code[b], v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= scale;
+            for (int i = 0; i < 8; ++i) k[i] = scale;
+            mul<8>(v, v, k);
             const int c = (quad * 4 + b) * 32 + q * 8;
             if (VEC) {
 #pragma unroll
@@ -164,10 +204,10 @@ int convert(bool quantize, void* data, void* scales, int rows, int cols, void* m
     a.x = m; a.y = m; a.data = static_cast<unsigned char*>(data); a.scales = static_cast<unsigned char*>(scales);
     a.ld = ld; a.rows = rows; a.cols = cols;
     a.blocks = 2 * ((cols + 63) / 64);
-    a.quads = (cols + 127) / 128;
-    a.units = up_div(rows, 8) * a.quads;
+    a.quads = tc_div((cols + 127) / 128);
+    a.units = up_div(rows, 8) * a.quads.d;
     const bool vec = (uintptr_t)m % 16 == 0 && (size_t)ld * elt % 16 == 0 && (size_t)cols * elt % 16 == 0;
-    const int blocks = (int)std::min<long long>(up_div(a.units, kThreads / 32), (long long)sms * 8);
+    const int blocks = (int)std::min<long long>(up_div(a.units, kThreads / 32), (long long)sms * 64);      // (short blocks: the scheduler balances them)
     const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     ALCS_CUDA(dt == ALCS_F32 ? launch<float>(quantize, vec, a, blocks, st) : dt == ALCS_F16 ? launch<__half>(quantize, vec, a, blocks, st)
                                                                                             : launch<__nv_bfloat16>(quantize, vec, a, blocks, st));
