@@ -50,6 +50,8 @@ struct Args {
     TcDiv cdiv, vdiv;            // by cg; by the loads of a group
     float eps;
     int relu, silu;
+    float *dgamma, *dbeta;
+    int first;                   // blocks in front of those that the kernel's own work is for (see back_apply_kernel)
 };
 
 // E neighbouring elements as they lie in memory.
@@ -263,8 +265,8 @@ struct Place {
     Place() = default;
     __device__ __forceinline__ explicit Place(const Args& a)
     {
-        const int unit = blockIdx.x / a.chunks;
-        rank = blockIdx.x - unit * a.chunks;
+        const int block = (int)blockIdx.x - a.first, unit = block / a.chunks;
+        rank = block - unit * a.chunks;
         img = unit / a.spans;
         span = unit - img * a.spans;
         ch0 = span * a.gs * a.cg;
@@ -895,15 +897,47 @@ __global__ void __launch_bounds__(kSplitThreads, 3) back_stats_kernel(const Args
     weigh<kSplitThreads, E>(at, a, gamma, rstd, sums, reinterpret_cast<float2*>(a.part) + ((size_t)at.img * a.chunks + at.rank) * a.groups + at.span * a.gs);
 }
 
+// dbeta and dgamma: sums[part][2][channel] over the n parts (blocks of images), channels 8 k to 8 k + 7 (32 bytes of a part), N / 8 parts side by side.
+template <int N>
+__device__ __forceinline__ void sum_params(float* s, const float* sums, float* dgamma, float* dbeta, int n, int c, int k8)
+{
+    constexpr int kRows = N / 8;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = threadIdx.x & 7, row = threadIdx.x >> 3, ch = k8 * 8 + k;
+    float u = 0.0f, w = 0.0f;
+    if (ch < c)
+#pragma unroll 8
+        for (int i = row; i < n; i += kRows) {
+            u += sums[(size_t)i * 2 * c + ch];
+            w += sums[((size_t)i * 2 + 1) * c + ch];
+        }
+    s[k * (kRows + 1) + row] = u;
+    s[(8 + k) * (kRows + 1) + row] = w;
+    __syncthreads();
+    for (int j = warp; j < 16; j += N / 32) {
+        float t = 0.0f;
+#pragma unroll
+        for (int r = 0; r < kRows; r += 32) t += s[j * (kRows + 1) + r + lane];
+        t = warp_sum(t);
+        float* const to = j >> 3 ? dgamma : dbeta;
+        const int out = k8 * 8 + (j & 7);
+        if (lane == 0 && out < c && to) to[out] = t;
+    }
+}
+
+// The first blocks sum dgamma and dbeta meanwhile.
 template <typename T, int E, bool SILU>
 __global__ void __launch_bounds__(kSplitThreads, 3) back_apply_kernel(const Args a)
 {
     extern __shared__ __align__(16) float ring[];
     __shared__ float k1[kMaxSpanGroups], k2[kMaxSpanGroups];
     void* const dring = reinterpret_cast<raw_t<T, E>*>(ring) + kDeepBack * kSplitThreads;
-    const Place<E, kSplitThreads> at(a);
     let_next_start();
     wait_for_previous();
+    if ((int)blockIdx.x < a.first) {
+        sum_params<kSplitThreads>(ring, a.sums, a.dgamma, a.dbeta, a.n * a.chunks, a.c, blockIdx.x);
+        return;
+    }
+    const Place<E, kSplitThreads> at(a);
     const size_t q0 = (size_t)at.img * a.groups + at.span * a.gs;
     const int l = lanes_of<kSplitThreads>(at.ng), sub_ = threadIdx.x & (l - 1);
     const float inv = 1.0f / ((float)a.hw * a.cg);
@@ -968,29 +1002,12 @@ __global__ void __launch_bounds__(kSplitThreads, 3) back_apply_kernel(const Args
     }
 }
 
-// dbeta and dgamma: sums[part][2][channel] over the parts (blocks of images), 8 channels per block (32 bytes of a part), 128 parts side by side.
 __global__ void __launch_bounds__(1024) params_kernel(const float* sums, float* dgamma, float* dbeta, int n, int c)
 {
-    __shared__ float s[2][8][129];
+    __shared__ float s[2 * 8 * (1024 / 8 + 1)];
     let_next_start();
     wait_for_previous();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = threadIdx.x & 7, row = threadIdx.x >> 3, ch = blockIdx.x * 8 + k;
-    float u = 0.0f, w = 0.0f;
-    if (ch < c)
-#pragma unroll 8
-        for (int i = row; i < n; i += 128) {
-            u += sums[(size_t)i * 2 * c + ch];
-            w += sums[((size_t)i * 2 + 1) * c + ch];
-        }
-    s[0][k][row] = u;
-    s[1][k][row] = w;
-    __syncthreads();
-    if (warp >= 16) return;
-    const float* const from = s[warp >> 3][warp & 7];
-    const float t = warp_sum(from[lane] + from[lane + 32] + (from[lane + 64] + from[lane + 96]));
-    float* const to = warp >> 3 ? dgamma : dbeta;
-    const int out = blockIdx.x * 8 + (warp & 7);
-    if (lane == 0 && out < c && to) to[out] = t;
+    sum_params<1024>(s, sums, dgamma, dbeta, n, c, blockIdx.x);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1149,7 +1166,10 @@ int run(Args& a, bool back, alcs_dtype dt, int dev, const NormPlan& p, void* wor
     if (rc) return rc;
     ALCS_CUDA(launch_pdl(first, grid, p.cluster ? kThreads : kSplitThreads, p.smem, std::max(1, p.cluster), st, a));
     if (p.cluster) return ALCS_OK;
-    ALCS_CUDA(launch_pdl(kernel_of(dt, p, back, 2, a.silu), grid, kSplitThreads, p.ring, 1, st, a));
+    if (back && (a.dgamma || a.dbeta)) a.first = (int)up_div(a.c, 8);
+    if (blocks + a.first > 0x7fffffffll) return ALCS_ERR_SHAPE;
+    ALCS_CUDA(launch_pdl(kernel_of(dt, p, back, 2, a.silu), dim3((unsigned)(blocks + a.first)), kSplitThreads, std::max(p.ring, (size_t)(back ? 16 * (kSplitThreads / 8 + 1) * 4 : 0)),
+                         1, st, a));
     return ALCS_OK;
 }
 
@@ -1236,10 +1256,11 @@ ALCS_API int alcs_group_norm_backward(const void* x, const void* dy, void* dx, i
         a.x = x; a.dy = dy; a.out = dx; a.gamma = gamma; a.beta = beta; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
         a.n = n; a.hw = hw; a.c = c; a.groups = groups; a.cg = c / groups;
         a.relu = (flags & ALCS_RELU) != 0; a.silu = (flags & ALCS_SILU) != 0;
+        a.dgamma = dgamma; a.dbeta = dbeta;
         rc = run(a, true, dt, dev, p, workspace, st);
         if (rc) return rc;
     }
-    if (dgamma || dbeta)
+    if ((dgamma || dbeta) && (none || p.cluster))
         ALCS_CUDA(launch_pdl(params_kernel, dim3((unsigned)up_div(c, 8)), 1024, 0, 1, st, static_cast<const float*>(workspace), dgamma, dbeta, none ? 0 : n * p.chunks, c));
     return ALCS_OK;
 }
