@@ -48,6 +48,8 @@ struct Args {
     int span_ch;                 // channels per span, rounded up to a multiple of 4
     int whole;                   // a load's channels lie in one group
     TcDiv cdiv, vdiv;            // by cg; by the loads of a group
+    TcDiv chdiv, spdiv;          // by chunks, spans
+    TcDiv nvdiv, rowdiv;         // of a span of gs groups: by its loads per pixel, by the pixels side by side in a block
     float eps;
     int relu, silu;
     float *dgamma, *dbeta;
@@ -254,6 +256,9 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
+// n / d as a multiplication (an integer division is 30 instructions, and there are ten per thread)
+__device__ __forceinline__ int over(int n, const TcDiv& d) { return (int)((unsigned long long)(unsigned)n * d.mul >> d.shift); }
+
 // Where a thread stands: its channels and pixels.
 template <int E, int N>
 struct Place {
@@ -262,37 +267,32 @@ struct Place {
     int rows, v, r;              // pixels side by side in the block; the thread's vector, pixel
     bool active;
     int p0, p1;                  // the block's pixels
-    Place() = default;
+    int loads;                   // the thread's, of a column of loads
     __device__ __forceinline__ explicit Place(const Args& a)
     {
-        const int block = (int)blockIdx.x - a.first, unit = block / a.chunks;
+        const int block = (int)blockIdx.x - a.first, unit = over(block, a.chdiv);
         rank = block - unit * a.chunks;
-        img = unit / a.spans;
+        img = over(unit, a.spdiv);
         span = unit - img * a.spans;
         ch0 = span * a.gs * a.cg;
         ng = min(a.gs, a.groups - span * a.gs);
         nch = ng * a.cg;
-        nv = nch / E;
-        rows = max(1, N / nv);
-        r = nv <= N ? threadIdx.x / nv : 0;
-        v = threadIdx.x - r * nv;
-        active = r < rows && v < nv;
         p0 = min(a.hw, rank * a.chunk);
         p1 = min(a.hw, p0 + a.chunk);
+        const bool whole = ng == a.gs;      // (the last span may have fewer)
+        nv = whole ? a.nvdiv.d : nch / E;
+        rows = whole ? a.rowdiv.d : max(1, N / nv);
+        r = nv > N ? 0 : whole ? over(threadIdx.x, a.nvdiv) : threadIdx.x / nv;
+        v = threadIdx.x - r * nv;
+        active = r < rows && v < nv;
+        const int mine = active ? max(0, p1 - p0 - r + rows - 1) : 0;
+        loads = whole ? over(mine, a.rowdiv) : mine / rows;
     }
 };
 
-// n / d of small numbers, d = a.cg
-__device__ __forceinline__ int over(int n, const TcDiv& d) { return (int)((unsigned long long)(unsigned)n * d.mul >> d.shift); }
-
-// Threads that share a group's values in the sums below: neighbouring lanes, as many as there are threads for.
+// Threads that share a group's values in the sums below: 2^k neighbouring lanes, as many as there are threads for.
 template <int N>
-__device__ __forceinline__ int lanes_of(int groups)
-{
-    int l = 32;
-    while (l > 1 && l * groups > N) l >>= 1;
-    return l;
-}
+__device__ __forceinline__ int lanes_of(int groups) { return min(5, 31 - __clz(max(1, N / groups))); }
 
 // n values of mean m and sum of squared distances q, united with as many again as `other` says
 struct Union {
@@ -350,8 +350,8 @@ __device__ __forceinline__ void unite(const Place<E, N>& at, const Args& a, int 
     __syncthreads();
     const int w = a.whole ? a.cg / E : a.cg;      // entries of a group in a row
     const float inv = at.p1 > at.p0 ? 1.0f / ((float)(at.p1 - at.p0) * a.cg) : 0.0f;
-    const int l = lanes_of<N>(at.ng), sub = threadIdx.x & (l - 1);
-    for (int g0 = threadIdx.x / l; g0 - (int)threadIdx.x / l < at.ng; g0 += N / l) {      // (all threads: their lanes exchange sums)
+    const int lk = lanes_of<N>(at.ng), l = 1 << lk, sub = threadIdx.x & (l - 1), mine = threadIdx.x >> lk;
+    for (int g0 = mine; g0 - mine < at.ng; g0 += N >> lk) {      // (all threads: their lanes exchange sums)
         const int g = min(g0, at.ng - 1);
         const float* const from = red + g * w;
         float s = 0.0f, t = 0.0f;
@@ -374,8 +374,8 @@ __device__ __forceinline__ void unite(const Place<E, N>& at, const Args& a, int 
 template <int N, int E>
 __device__ __forceinline__ void weigh(const Place<E, N>& at, const Args& a, const float* gamma, const float* rstd, const float* sums, float2* out)
 {
-    const int l = lanes_of<N>(at.ng), sub = threadIdx.x & (l - 1);
-    for (int g0 = threadIdx.x / l; g0 - (int)threadIdx.x / l < at.ng; g0 += N / l) {
+    const int lk = lanes_of<N>(at.ng), l = 1 << lk, sub = threadIdx.x & (l - 1), mine = threadIdx.x >> lk;
+    for (int g0 = mine; g0 - mine < at.ng; g0 += N >> lk) {
         const int g = min(g0, at.ng - 1);
         float s1 = 0.0f, s2 = 0.0f;
         for (int j = sub; j < a.cg; j += l) {
@@ -459,7 +459,7 @@ __global__ void __launch_bounds__(kThreads, 8) norm_kernel(const Args a)
     let_next_start();
     wait_for_previous();
     const size_t first = ((size_t)at.img * a.hw + at.p0 + at.r) * a.c + at.ch0 + ch, step = (size_t)at.rows * a.c;
-    const int n = at.active ? max(0, at.p1 - at.p0 - at.r + at.rows - 1) / at.rows : 0;      // loads
+    const int n = at.loads;
     fetch<T, E>(slot, static_cast<const T*>(a.x) + first, step, n);
     for (int i = threadIdx.x; i < at.nch; i += kThreads) {
         scale[i] = a.gamma ? __ldg(a.gamma + at.ch0 + i) : 1.0f;
@@ -494,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 8) norm_kernel(const Args a)
     const float total = 1.0f / ((float)a.hw * a.cg);
     const int lane = threadIdx.x & 31;
     for (int i = threadIdx.x; i - lane < at.ng * a.chunks; i += kThreads) {
-        const int g = min(i / a.chunks, at.ng - 1), r = i & (a.chunks - 1);      // (chunks: a power of two, at most 16)
+        const int g = min(over(i, a.chdiv), at.ng - 1), r = i & (a.chunks - 1);      // (chunks: a power of two, at most 16)
         const float w = (float)pixels_of(a, r) * a.cg;
         const float2 o = a.chunks > 1 ? ld_rank(own + g, r) : own[g];
         const float mu = w > 0.0f ? lanes_sum(o.x * w, a.chunks) * total : lanes_sum(0.0f, a.chunks) * total;
@@ -555,7 +555,7 @@ __global__ void __launch_bounds__(kThreads, 6) norm_back_kernel(const Args a)
     let_next_start();
     wait_for_previous();
     const size_t first = ((size_t)at.img * a.hw + at.p0 + at.r) * a.c + at.ch0 + ch, step = (size_t)at.rows * a.c;
-    const int n = at.active ? max(0, at.p1 - at.p0 - at.r + at.rows - 1) / at.rows : 0;
+    const int n = at.loads;
     fetch<T, E>(slot, static_cast<const T*>(a.x) + first, step, n);
     fetch<T, E>(dslot, static_cast<const T*>(a.dy) + first, step, n);
     for (int i = threadIdx.x; i < at.nch; i += kThreads) {
@@ -600,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, 6) norm_back_kernel(const Args a)
     else __syncthreads();
     const float inv = 1.0f / ((float)a.hw * a.cg);
     for (int i = threadIdx.x; i - lane < at.ng * a.chunks; i += kThreads) {
-        const int q = min(i / a.chunks, at.ng - 1), k = i & (a.chunks - 1);
+        const int q = min(over(i, a.chdiv), at.ng - 1), k = i & (a.chunks - 1);
         const float2 o = a.chunks > 1 ? ld_rank(own + q, k) : own[q];
         const float r = rstd[q * a.cg];
         const float s1 = lanes_sum(o.x, a.chunks) * inv * -r, s2 = lanes_sum(o.y, a.chunks) * inv * -r * r;
@@ -699,7 +699,7 @@ __global__ void __launch_bounds__(kSplitThreads, 4) stats_kernel(const Args a)
     for (int v = at.v; at.active && v < at.nv; v += kSplitThreads) {
         const T* x = static_cast<const T*>(a.x) + ((size_t)at.img * a.hw + at.p0 + at.r) * a.c + at.ch0 + v * E;
         const size_t step = (size_t)at.rows * a.c;
-        const int loads = (at.p1 - at.p0 - at.r + at.rows - 1) / at.rows;
+        const int loads = at.loads;
         Column<T, E, kDeep> col(ring, x, step);
 #pragma unroll
         for (int j = 0; j < kDeep; ++j) { col.ask(j, j < loads); asked(); }
@@ -775,9 +775,9 @@ __global__ void __launch_bounds__(kSplitThreads, 4) apply_kernel(const Args a)
     const Place<E, kSplitThreads> at(a);
     let_next_start();
     wait_for_previous();
-    const int l = lanes_of<kSplitThreads>(at.ng), sub_ = threadIdx.x & (l - 1);
+    const int lk = lanes_of<kSplitThreads>(at.ng), l = 1 << lk, sub_ = threadIdx.x & (l - 1), mine = threadIdx.x >> lk;
     const float total = (float)a.hw * a.cg;
-    for (int g0 = threadIdx.x / l; g0 - (int)threadIdx.x / l < at.ng; g0 += kSplitThreads / l) {
+    for (int g0 = mine; g0 - mine < at.ng; g0 += kSplitThreads >> lk) {
         const int g = min(g0, at.ng - 1);
         const float2* const from = reinterpret_cast<const float2*>(a.part) + (size_t)at.img * a.chunks * a.groups + at.span * a.gs + g;
         float s = 0.0f, m2 = 0.0f;
@@ -806,7 +806,7 @@ __global__ void __launch_bounds__(kSplitThreads, 4) apply_kernel(const Args a)
         const size_t step = (size_t)at.rows * a.c;
         const T* x = static_cast<const T*>(a.x) + first;
         T* y = static_cast<T*>(a.out) + first;
-        const int loads = (at.p1 - at.p0 - at.r + at.rows - 1) / at.rows;
+        const int loads = at.loads;
         Column<T, E, kDeep> col(ring, x, step);
 #pragma unroll
         for (int j = 0; j < kDeep; ++j) { col.ask(j, j < loads); asked(); }
@@ -859,7 +859,7 @@ __global__ void __launch_bounds__(kSplitThreads, 3) back_stats_kernel(const Args
         const size_t first = ((size_t)at.img * a.hw + at.p0 + at.r) * a.c + at.ch0 + v * E, step = (size_t)at.rows * a.c;
         const T* x = static_cast<const T*>(a.x) + first;
         const T* dy = static_cast<const T*>(a.dy) + first;
-        const int loads = (at.p1 - at.p0 - at.r + at.rows - 1) / at.rows;
+        const int loads = at.loads;
         Column<T, E, kDeepBack> col(ring, x, step), dcol(dring, dy, step);
 #pragma unroll
         for (int j = 0; j < kDeepBack; ++j) { col.ask(j, j < loads); dcol.ask(j, j < loads); asked(); }
@@ -939,9 +939,9 @@ __global__ void __launch_bounds__(kSplitThreads, 3) back_apply_kernel(const Args
     }
     const Place<E, kSplitThreads> at(a);
     const size_t q0 = (size_t)at.img * a.groups + at.span * a.gs;
-    const int l = lanes_of<kSplitThreads>(at.ng), sub_ = threadIdx.x & (l - 1);
+    const int lk = lanes_of<kSplitThreads>(at.ng), l = 1 << lk, sub_ = threadIdx.x & (l - 1), mine = threadIdx.x >> lk;
     const float inv = 1.0f / ((float)a.hw * a.cg);
-    for (int g0 = threadIdx.x / l; g0 - (int)threadIdx.x / l < at.ng; g0 += kSplitThreads / l) {
+    for (int g0 = mine; g0 - mine < at.ng; g0 += kSplitThreads >> lk) {
         const int g = min(g0, at.ng - 1);
         const float2* const from = reinterpret_cast<const float2*>(a.part) + (size_t)at.img * a.chunks * a.groups + at.span * a.gs + g;
         float s1 = 0.0f, s2 = 0.0f;
@@ -974,7 +974,7 @@ __global__ void __launch_bounds__(kSplitThreads, 3) back_apply_kernel(const Args
         const T* x = static_cast<const T*>(a.x) + first;
         const T* dy = static_cast<const T*>(a.dy) + first;
         T* dx = static_cast<T*>(a.out) + first;
-        const int loads = (at.p1 - at.p0 - at.r + at.rows - 1) / at.rows;
+        const int loads = at.loads;
         Column<T, E, kDeepBack> col(ring, x, step), dcol(dring, dy, step);
 #pragma unroll
         for (int j = 0; j < kDeepBack; ++j) { col.ask(j, j < loads); dcol.ask(j, j < loads); asked(); }
@@ -1160,6 +1160,11 @@ int run(Args& a, bool back, alcs_dtype dt, int dev, const NormPlan& p, void* wor
     a.whole = a.cg % p.e == 0;
     a.cdiv = tc_div(a.cg);
     a.vdiv = tc_div(std::max(1, a.cg / p.e));
+    a.chdiv = tc_div(a.chunks);
+    a.spdiv = tc_div(a.spans);
+    const int nv = a.gs * a.cg / p.e;
+    a.nvdiv = tc_div(nv);
+    a.rowdiv = tc_div(std::max(1, (p.cluster ? kThreads : kSplitThreads) / nv));
     const dim3 grid((unsigned)blocks);
     const Kernel first = kernel_of(dt, p, back, p.cluster ? 0 : 1, a.silu);
     const int rc = allow((const void*)first, p.smem, p.cluster, dev);
