@@ -457,8 +457,8 @@ ALCS_API int alcs_spconv2d_plan(const alcs_packed* w, int n, int cin, int h, int
  *     z = gamma[channel] * xh + beta[channel],  y = act(z),  act the identity, ALCS_RELU or ALCS_SILU (flags).
  * x and y are device [n][h*wd][c] (NHWC), contiguous, of type dt, aligned to their element size; y may be x itself, but not
  * overlap it otherwise.  gamma and beta are device fp32 [c] or NULL (1 and 0); mean and rstd receive mu and rstd, device fp32
- * [n][groups], or are NULL.  Statistics and everything up to the rounding of y are fp32; squares are summed
- * of values less one of a few dozen neighbours, and of differences of means, so that a mean far from 0 costs no accuracy.  An infinity
+ * [n][groups], or are NULL.  Statistics and everything up to the rounding of y are fp32; the variance comes from
+ * running means and differences of means, so that a mean far from 0 costs no accuracy.  An infinity
  * or NaN makes its group of its image NaN.  ReLU turns NaN into 0, as in the convolutions.
  *
  * alcs_group_norm_backward: for the derivative dy of a loss by y, with dz = dy * act'(z) (act' of ReLU at 0 is 0) and t = gamma * dz,

@@ -10,15 +10,16 @@
 // of a pixel where that is possible: whole sectors of memory) of one image; its pixels are shared out to the blocks of a cluster, and a block holds its
 // share in shared memory, which cp.async fills without holding registers.  A thread keeps to its channels.  Sums go through shared memory, in a fixed
 // order, and between the cluster's blocks through distributed shared memory.  What it costs over a copy is the sums: all blocks of an SM tend to be at them
-// at the same time, with memory idle (64 images of 56x56x128, bf16: 33 us; a copy of them 18; without the sums 20; floor 15.7 at 6.5 TB/s).
+// at the same time, with memory idle (64 images of 56x56x128, bf16: 29.5 us among other calls; a copy of them 22.5; the same
+// kernel without the sums 24.6; floor 15.7 at 6.5 TB/s).
 //
 // Two passes: sums of chunks of pixels, then the outputs from a second reading, which L2 serves as far as it holds x (and dy).  For spans that do
 // not fit a cluster, and for large calls of the backward pass.  Every thread keeps 8 loads (4 of x and dy each) on their way to slots of its own in
-// shared memory: with as many registers instead, a third of the bytes were in flight (backward of 64 images of 56x56x256, SiLU: 143 us, then 105:
-// 46 and 51 us for the passes).
+// shared memory: with as many registers instead, a third of the bytes were in flight (backward of 64 images of 56x56x256, SiLU: 143 us, then 105;
+// 46 and 51 us for the passes now).
 //
-// The variance is that of values with a mean taken off: a thread's run of at most 32 loads (one pass: what it holds) is summed less its first value, runs are
-// united by M2 = M2_a + M2_b + n_a n_b / n (mean_a - mean_b)^2, which has no cancellation where the mean is large.  All of it in fp32.
+// The variance has no cancellation: a thread takes its values one by one into a running mean and sum of squared distances, and these are united by
+// M2 = M2_a + M2_b + n_a n_b / n (mean_a - mean_b)^2.  All of it in fp32.
 #include <algorithm>
 #include <cmath>
 #include <mutex>
@@ -294,6 +295,29 @@ struct Place {
 template <int N>
 __device__ __forceinline__ int lanes_of(int groups) { return min(5, 31 - __clz(max(1, N / groups))); }
 
+// Mean and sum of squared distances from it, value by value (Welford's recurrence, E channels side by side): one operation more per value than sums of values
+// less one of them, and no loss where that one is far from the others.
+template <int E>
+struct Running {
+    float m[E], q[E], n = 0.0f;
+    __device__ __forceinline__ Running()
+    {
+        set<E>(m, 0.0f);
+        set<E>(q, 0.0f);
+    }
+    __device__ __forceinline__ void take(float (&v)[E])
+    {
+        n += 1.0f;
+        float r, d[E], k[E];
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(n));      // (the mean's steps need no more)
+        set<E>(k, r);
+        sub<E>(d, v, m);
+        fma<E>(m, d, k, m);
+        sub<E>(v, v, m);
+        fma<E>(q, d, v, q);
+    }
+};
+
 // n values of mean m and sum of squared distances q, united with as many again as `other` says
 struct Union {
     float to, both;      // share of the other's; n times it
@@ -309,11 +333,11 @@ struct Union {
 // Mean and sum of squared distances from it of the block's values of every group of the span: out[group].  A thread has n values of mean m and
 // squared distances q per channel.  `red`: 2 E floats per thread, `count`: one per thread.
 template <int N, int E>
-__device__ __forceinline__ void unite(const Place<E, N>& at, const Args& a, int n, float (&m)[E], float (&q)[E], float* red, float* count, float2* out)
+__device__ __forceinline__ void unite(const Place<E, N>& at, const Args& a, float n, float (&m)[E], float (&q)[E], float* red, float* count, float2* out)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const bool lanes = at.nv < 32 && (at.nv & (at.nv - 1)) == 0;       // lanes nv apart have the same vector
-    float k = (float)n;
+    float k = n;
     if (a.whole && E > 1) {      // the thread's channels are one group's
         float s = 0.0f, t = 0.0f;
 #pragma unroll
@@ -466,28 +490,14 @@ __global__ void __launch_bounds__(kThreads, 8) norm_kernel(const Args a)
         shift[i] = a.beta ? __ldg(a.beta + at.ch0 + i) : 0.0f;
     }
     fetched();
-    // Sums of the thread's values, and of their squares, less the first one: of n values the square of the mean is then at most n times the
-    // sum of squared distances, and n is small.
-    float k[E], s[E], q[E];
-    set<E>(s, 0.0f);
-    set<E>(q, 0.0f);
-    if (n) get<T, E>(slot[0], k);
+    Running<E> stat;
 #pragma unroll 4
-    for (int i = 1; i < n; ++i) {
+    for (int i = 0; i < n; ++i) {
         float v[E];
         get<T, E>(slot[i * kThreads], v);
-        sub<E>(v, v, k);
-        add<E>(s, s, v);
-        fma<E>(q, v, v, q);
+        stat.take(v);
     }
-    const float inv = n ? 1.0f / (float)n : 0.0f;
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-        const float d = s[j] * inv;
-        q[j] = fmaxf(fmaf(-d, s[j], q[j]), 0.0f * q[j]);      // (a NaN stays one)
-        s[j] = n ? k[j] + d : 0.0f;                           // the thread's mean
-    }
-    unite<kThreads, E>(at, a, n, s, q, red, count, own);
+    unite<kThreads, E>(at, a, stat.n, stat.m, stat.q, red, count, own);
     if (a.chunks > 1) cluster_sync();
     else __syncthreads();
     // Every block unites the cluster's, a lane per (group, block), and spreads a group's result over its channels.
@@ -517,15 +527,16 @@ __global__ void __launch_bounds__(kThreads, 8) norm_kernel(const Args a)
     if (a.chunks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // done with the others' shared memory
     if (n) {
         T* y = static_cast<T*>(a.out) + first;
-        load_shared<E>(k, mean + ch);
+        float m[E], s[E], b[E];
+        load_shared<E>(m, mean + ch);
         load_shared<E>(s, scale + ch);
-        load_shared<E>(q, shift + ch);
+        load_shared<E>(b, shift + ch);
 #pragma unroll 2
         for (int i = 0; i < n; ++i, y += step) {
             float v[E];
             get<T, E>(slot[i * kThreads], v);
-            sub<E>(v, v, k);
-            fma<E>(v, v, s, q);
+            sub<E>(v, v, m);
+            fma<E>(v, v, s, b);
             activate<SILU, E>(v, a.relu);
             store<T, E>(y, v);
         }
@@ -656,8 +667,6 @@ __device__ __forceinline__ void channels(const Args& a, int ch0, int ch, const f
     }
 }
 
-constexpr int kRun = 32;       // loads whose squares are summed less the first one's (a multiple of kDeep)
-
 // A thread's column of n loads, D of them on their way to its slots of shared memory [D][thread]: for a kernel that keeps no more of what it reads, registers
 // would hold too few loads in flight.  Loops are unrolled D times, so that a slot's place is known.
 template <typename T, int E, int D>
@@ -692,9 +701,7 @@ __global__ void __launch_bounds__(kSplitThreads, 4) stats_kernel(const Args a)
     const Place<E, kSplitThreads> at(a);
     let_next_start();
     wait_for_previous();
-    float s[E], q[E], n = 0.0f;
-    set<E>(s, 0.0f);
-    set<E>(q, 0.0f);
+    Running<E> stat;
     const bool wide = at.nv > kSplitThreads;
     for (int v = at.v; at.active && v < at.nv; v += kSplitThreads) {
         const T* x = static_cast<const T*>(a.x) + ((size_t)at.img * a.hw + at.p0 + at.r) * a.c + at.ch0 + v * E;
@@ -703,66 +710,47 @@ __global__ void __launch_bounds__(kSplitThreads, 4) stats_kernel(const Args a)
         Column<T, E, kDeep> col(ring, x, step);
 #pragma unroll
         for (int j = 0; j < kDeep; ++j) { col.ask(j, j < loads); asked(); }
-        for (int i0 = 0; i0 < loads; i0 += kRun) {
-            float f[E], u[E], w[E];      // (as norm_kernel: less the first value, of a short run)
-            set<E>(u, 0.0f);
-            set<E>(w, 0.0f);
-            const int end = min(loads, i0 + kRun);
-            wait_oldest<kDeep>();
-            get<T, E>(col.at(0), f);
-            for (int i = i0; i < end; i += kDeep)
+        for (int i = 0; i < loads; i += kDeep)
 #pragma unroll
-                for (int j = 0; j < kDeep; ++j)
-                    if (i + j < end) {
-                        wait_oldest<kDeep>();
-                        float d[E];
-                        get<T, E>(col.at(j), d);
-                        sub<E>(d, d, f);
-                        add<E>(u, u, d);
-                        fma<E>(w, d, d, w);
-                        col.ask(j, i + j + kDeep < loads);
-                        asked();
-                    }
-            const float run = (float)(end - i0), inv = 1.0f / run;
-            const Union both(n, run);
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const float d = u[j] * inv;
-                w[j] = fmaxf(fmaf(-d, u[j], w[j]), 0.0f * w[j]);
-                both(s[j], q[j], f[j] + d, w[j]);
-            }
-            n += run;
-        }
+            for (int j = 0; j < kDeep; ++j)
+                if (i + j < loads) {
+                    wait_oldest<kDeep>();
+                    float d[E];
+                    get<T, E>(col.at(j), d);
+                    stat.take(d);
+                    col.ask(j, i + j + kDeep < loads);
+                    asked();
+                }
     }
     float2* const to = reinterpret_cast<float2*>(a.part) + ((size_t)at.img * a.chunks + at.rank) * a.groups + at.span * a.gs;
     if (!wide) {
-        unite<kSplitThreads, E>(at, a, (int)n, s, q, red, count, to);
+        unite<kSplitThreads, E>(at, a, stat.n, stat.m, stat.q, red, count, to);
         return;
     }
     // one group: all of the block's values
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float c = n;
+    float c = stat.n;
 #pragma unroll
     for (int j = 1; j < E; ++j) {
-        const Union both(c, n);
-        both(s[0], q[0], s[j], q[j]);
-        c += n;
+        const Union both(c, stat.n);
+        both(stat.m[0], stat.q[0], stat.m[j], stat.q[j]);
+        c += stat.n;
     }
     for (int o = 1; o < 32; o <<= 1) {
         const float other = __shfl_xor_sync(0xffffffffu, c, o);
         const Union both(c, other);
-        both(s[0], q[0], __shfl_xor_sync(0xffffffffu, s[0], o), __shfl_xor_sync(0xffffffffu, q[0], o));
+        both(stat.m[0], stat.q[0], __shfl_xor_sync(0xffffffffu, stat.m[0], o), __shfl_xor_sync(0xffffffffu, stat.q[0], o));
         c += other;
     }
-    if (lane == 0) { red[warp] = s[0]; red[32 + warp] = q[0]; count[warp] = c; }
+    if (lane == 0) { red[warp] = stat.m[0]; red[32 + warp] = stat.q[0]; count[warp] = c; }
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < kSplitThreads / 32; ++i) {
             const Union both(c, count[i]);
-            both(s[0], q[0], red[i], red[32 + i]);
+            both(stat.m[0], stat.q[0], red[i], red[32 + i]);
             c += count[i];
         }
-        *to = make_float2(s[0], q[0]);
+        *to = make_float2(stat.m[0], stat.q[0]);
     }
 }
 
@@ -1065,7 +1053,7 @@ NormPlan make_plan(int n, int hw, int c, int groups, int elt, int align, bool ba
     while (p.gs * 2 <= std::min(kMaxSpanGroups, groups) && (long long)p.gs * 2 * cg / p.e <= kSplitThreads) p.gs *= 2;
     const long long units = (long long)n * up_div(groups, p.gs);
     const long long nv = (long long)p.gs * cg / p.e, rows = std::max<long long>(1, kSplitThreads / nv);
-    // Long columns of a thread's loads, as far as every SM has work; and short enough for sums of squares less one of the values.
+    // Long columns of a thread's loads, as far as every SM has work.
     const long long loads = std::max(4ll, std::min(32ll, up_div(up_div(hw, rows) * units, 4ll * sms)));
     p.chunks = (int)std::min(up_div(hw, rows * loads), 4096ll);
     p.chunk = (int)up_div(hw, p.chunks);

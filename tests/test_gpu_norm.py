@@ -159,6 +159,22 @@ def test_a_mean_far_from_zero(alcs, shape):
     assert np.abs(f64(k.rstd) / ref["rstd"] - 1).max() <= 128 * 2.0 ** -24 + (64 * 2.0 ** -24 * 1001) ** 2
 
 
+@pytest.mark.parametrize("shape", [(1, 30, 30, 64, 8), (2, 41, 37, 35, 5), (1, 150, 120, 64, 2), (1, 60, 50, 1031, 1), (1, 120, 120, 31, 31)])
+def test_an_outlier_where_a_thread_or_a_block_starts(alcs, shape):
+    """10^4 among values of order 1, at the first and at some other pixel: the variance is theirs, to the rounding of its sums."""
+    n, h, w, c, groups = shape
+    x, dy, gamma, beta = _inputs(7, n, h * w, c, "f32", alcs)
+    x[:, 0] += 1e4
+    x[:, 57] -= 2e4
+    k = Norm(alcs, x, shape, "f32", "none", 1e-5, gamma, beta)
+    y = f64(k.forward())
+    ref = dense.group_norm(f64(x), groups, f64(gamma), f64(beta))
+    _within(y, ref["y"], norm_bound(ref, f64(x), f64(gamma), f64(beta), groups, "f32"))
+    # A sum of squared distances is rounded once at each of a thread's values (at most 32 loads of 5 vectors), twice at each of some 15 unions, and a term of
+    # it has 6 roundings of its own: 196 x 2^-24, half of that in rstd.
+    assert np.abs(f64(k.rstd) / ref["rstd"] - 1).max() <= 98 * 2.0 ** -24
+
+
 def test_constant_groups_and_eps(alcs):
     import torch
     x = torch.full((1, 25, 32), 7.0, device="cuda")
