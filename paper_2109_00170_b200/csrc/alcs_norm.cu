@@ -318,15 +318,16 @@ struct Running {
     }
 };
 
-// n values of mean m and sum of squared distances q, united with as many again as `other` says
+// n values of mean m and sum of squared distances q, united with as many again as `other` says.  Either may be none (m = q = 0): the distance of the means then
+// is the size of a value, whose square may not be a number of fp32 (0 times which is NaN), and is multiplied by 0 before it is squared.
 struct Union {
-    float to, both;      // share of the other's; n times it
-    __device__ __forceinline__ Union(float n, float other) : to(n + other > 0.0f ? other / (n + other) : 0.0f), both(n * to) {}
+    float n, to;      // to: share of the other's
+    __device__ __forceinline__ Union(float n_, float other) : n(n_), to(n + other > 0.0f ? other / (n + other) : 0.0f) {}
     __device__ __forceinline__ void operator()(float& m, float& q, float om, float oq) const
     {
         const float d = om - m;
         m = fmaf(d, to, m);
-        q += fmaf(d * d, both, oq);
+        q += fmaf(d * to, d * n, oq);
     }
 };
 
@@ -509,8 +510,8 @@ __global__ void __launch_bounds__(kThreads, 8) norm_kernel(const Args a)
         const float2 o = a.chunks > 1 ? ld_rank(own + g, r) : own[g];
         const float mu = w > 0.0f ? lanes_sum(o.x * w, a.chunks) * total : lanes_sum(0.0f, a.chunks) * total;
         const float d = o.x - mu;
-        const float m2 = lanes_sum(w > 0.0f ? fmaf(d * d, w, o.y) : 0.0f, a.chunks);
-        const float rs = 1.0f / sqrtf(fmaf(m2, total, a.eps));
+        const float var = lanes_sum(w > 0.0f ? fmaf(d * d, w * total, o.y * total) : 0.0f, a.chunks);      // (each part's share: less than their sum)
+        const float rs = 1.0f / sqrtf(var + a.eps);
         if (i < at.ng * a.chunks) {
             for (int j = r; j < a.cg; j += a.chunks) {
                 mean[g * a.cg + j] = mu;
@@ -768,16 +769,16 @@ __global__ void __launch_bounds__(kSplitThreads, 4) apply_kernel(const Args a)
     for (int g0 = mine; g0 - mine < at.ng; g0 += kSplitThreads >> lk) {
         const int g = min(g0, at.ng - 1);
         const float2* const from = reinterpret_cast<const float2*>(a.part) + (size_t)at.img * a.chunks * a.groups + at.span * a.gs + g;
-        float s = 0.0f, m2 = 0.0f;
+        float s = 0.0f, var = 0.0f;
         for (int k = sub_; k < a.chunks; k += l) s = fmaf(from[(size_t)k * a.groups].x, (float)pixels_of(a, k) * a.cg, s);
         const float m = lanes_sum(s, l) / total;
         for (int k = sub_; k < a.chunks; k += l) {
             const float2 o = from[(size_t)k * a.groups];
-            m2 += fmaf((o.x - m) * (o.x - m), (float)pixels_of(a, k) * a.cg, o.y);
+            var += fmaf((o.x - m) * (o.x - m), (float)pixels_of(a, k) * a.cg / total, o.y / total);      // (each chunk's share: less than their sum)
         }
-        m2 = lanes_sum(m2, l);
+        var = lanes_sum(var, l);
         if (sub_ == 0 && g == g0) {
-            const float r = 1.0f / sqrtf(m2 / total + a.eps);
+            const float r = 1.0f / sqrtf(var + a.eps);
             mean[g] = m;
             rstd[g] = r;
             const size_t o = (size_t)at.img * a.groups + at.span * a.gs + g;

@@ -175,6 +175,22 @@ def test_an_outlier_where_a_thread_or_a_block_starts(alcs, shape):
     assert np.abs(f64(k.rstd) / ref["rstd"] - 1).max() <= 98 * 2.0 ** -24
 
 
+@pytest.mark.parametrize("spread", [0.0, 2.0 ** -10])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 1, 1, 64, 16), (2, 1, 3, 7, 7), (2, 5, 5, 96, 12), (3, 7, 7, 150, 30), (1, 150, 121, 64, 2), (1, 5, 4, 3001, 1)])
+def test_values_whose_squares_are_beyond_fp32(alcs, shape, dtype, spread):
+    """Around 2^66, apart by up to 2^56 or so: what is squared is distances between them, also where a thread has no value of its own."""
+    import torch
+    n, h, w, c, groups = shape
+    x, _, gamma, beta = _inputs(8, n, h * w, c, "f32", alcs, 0.0)
+    x = ((1 + spread * x) * 2.0 ** 66).to(types(alcs)[dtype][1])
+    k = Norm(alcs, x, shape, dtype, "none", 1e-5, gamma, beta)
+    y = f64(k.forward())
+    ref = dense.group_norm(f64(x), groups, f64(gamma), f64(beta))
+    _within(y, ref["y"], norm_bound(ref, f64(x), f64(gamma), f64(beta), groups, dtype))
+    assert np.abs(f64(k.mean) / 2.0 ** 66 - 1).max() <= 2.0 ** -8 and torch.isfinite(k.rstd).all()      # (means of a few values off by up to 5 x 2^-10)
+
+
 def test_constant_groups_and_eps(alcs):
     import torch
     x = torch.full((1, 25, 32), 7.0, device="cuda")
