@@ -458,8 +458,9 @@ ALCS_API int alcs_spconv2d_plan(const alcs_packed* w, int n, int cin, int h, int
  * x and y are device [n][h*wd][c] (NHWC), contiguous, of type dt, aligned to their element size; y may be x itself, but not
  * overlap it otherwise.  gamma and beta are device fp32 [c] or NULL (1 and 0); mean and rstd receive mu and rstd, device fp32
  * [n][groups], or are NULL.  Statistics and everything up to the rounding of y are fp32; the variance comes from
- * running means and differences of means, so that a mean far from 0 costs no accuracy.  An infinity
- * or NaN makes its group of its image NaN.  ReLU turns NaN into 0, as in the convolutions.
+ * running means and differences of means, so that a mean far from 0 costs no accuracy but its own rounding to fp32.  An infinity
+ * or NaN makes its group of its image NaN.  ReLU turns NaN into 0, as in the convolutions.  SiLU takes exp(-z) as 2^62 where it is more, so
+ * that y is z * 2^-62 for z below -43.
  *
  * alcs_group_norm_backward: for the derivative dy of a loss by y, with dz = dy * act'(z) (act' of ReLU at 0 is 0) and t = gamma * dz,
  *     dbeta = sum dz,  dgamma = sum dz * xh  (over images and pixels),
@@ -475,7 +476,7 @@ ALCS_API int alcs_spconv2d_plan(const alcs_packed* w, int n, int cin, int h, int
  * h*wd == 0 is a successful no-op, but for dgamma and dbeta, which become 0.
  * Errors: INVALID_ARG (null, misaligned or overlapping buffers, host memory, negative sizes, groups < 1, an eps that is negative or not finite, both
  * activations, workspace too small), SHAPE (c not a multiple of groups, h*wd or n*c of 2^30 and more, c above 65536),
- * UNSUPPORTED (more than 8192 channels per group), STATE (memory of another device), CUDA.
+ * UNSUPPORTED (more than 8192 channels per group), STATE (memory of another device), ALLOC (host), CUDA.
  * ------------------------------------------------------------------------------------------- */
 ALCS_API size_t alcs_group_norm_workspace(int n, int h, int wd, int c, int groups, alcs_dtype dt);
 ALCS_API int alcs_group_norm(const void* x, void* y, int n, int h, int wd, int c, int groups, const float* gamma, const float* beta,

@@ -1121,7 +1121,7 @@ int align_of(std::initializer_list<const void*> ps)
 
 // Shared memory beyond 48 KB (with a kernel's own) and clusters of 16, allowed once per kernel and device.
 int allow(const void* fn, size_t smem, int cluster, int dev)
-{
+try {
     static std::mutex mu;
     static std::set<std::pair<const void*, int>> allowed;
     if (smem <= 40 * 1024 && cluster <= 8) return ALCS_OK;
@@ -1131,6 +1131,8 @@ int allow(const void* fn, size_t smem, int cluster, int dev)
     ALCS_CUDA(cudaFuncSetAttribute(fn, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     allowed.insert({fn, dev});
     return ALCS_OK;
+} catch (const std::exception&) {      // no memory for an entry
+    return ALCS_ERR_ALLOC;
 }
 
 int run(Args& a, bool back, alcs_dtype dt, int dev, const NormPlan& p, void* workspace, cudaStream_t st)
