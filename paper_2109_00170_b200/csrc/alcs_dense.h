@@ -122,6 +122,21 @@ __device__ __forceinline__ void from_f32(float* p, float v) { *p = v; }
 __device__ __forceinline__ void from_f32(__half* p, float v) { *p = __float2half_rn(v); }
 __device__ __forceinline__ void from_f32(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
+// max(v, 0) of packed values, NaN to 0 (of rounded values: the rounding keeps their sign)
+__device__ __forceinline__ unsigned positive(unsigned v, __half)
+{
+    const __half2 z = __hmax2(reinterpret_cast<const __half2&>(v), __float2half2_rn(0.0f));
+    return reinterpret_cast<const unsigned&>(z);
+}
+__device__ __forceinline__ unsigned positive(unsigned v, __nv_bfloat16)
+{
+    const __nv_bfloat162 z = __hmax2(reinterpret_cast<const __nv_bfloat162&>(v), __float2bfloat162_rn(0.0f));
+    return reinterpret_cast<const unsigned&>(z);
+}
+__device__ __forceinline__ unsigned positive(unsigned v, float) { return __float_as_uint(fmaxf(__uint_as_float(v), 0.0f)); }
+template <typename T>
+__device__ __forceinline__ uint4 positive(const uint4& v, T t) { return make_uint4(positive(v.x, t), positive(v.y, t), positive(v.z, t), positive(v.w, t)); }
+
 // d = a + b, a - b, a * b, a * b + c on E elements, two per instruction.
 #define ALCS_PAIRS(name, op)                                                                                                                            \
     template <int E>                                                                                                                                    \

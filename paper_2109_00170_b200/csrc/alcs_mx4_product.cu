@@ -134,21 +134,6 @@ __device__ __forceinline__ void store_one(const Args& a, size_t at, float v, flo
     from_f32(static_cast<T*>(a.y) + at, v);
 }
 
-// max(v, 0) of packed values, NaN to 0 (of rounded values: the rounding keeps their sign)
-__device__ __forceinline__ unsigned positive(unsigned v, __half)
-{
-    const __half2 z = __hmax2(reinterpret_cast<const __half2&>(v), __float2half2_rn(0.0f));
-    return reinterpret_cast<const unsigned&>(z);
-}
-__device__ __forceinline__ unsigned positive(unsigned v, __nv_bfloat16)
-{
-    const __nv_bfloat162 z = __hmax2(reinterpret_cast<const __nv_bfloat162&>(v), __float2bfloat162_rn(0.0f));
-    return reinterpret_cast<const unsigned&>(z);
-}
-__device__ __forceinline__ unsigned positive(unsigned v, float) { return __float_as_uint(fmaxf(__uint_as_float(v), 0.0f)); }
-template <typename T>
-__device__ __forceinline__ uint4 positive(const uint4& v, T t) { return make_uint4(positive(v.x, t), positive(v.y, t), positive(v.z, t), positive(v.w, t)); }
-
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
 {

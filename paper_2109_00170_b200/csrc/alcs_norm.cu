@@ -32,7 +32,7 @@ namespace alcs {
 namespace {
 
 constexpr int kThreads = 128, kSplitThreads = 256;      // one pass; two passes
-constexpr int kMaxCluster = 16;
+constexpr int kMaxCluster = 16, kMostThreads = 1024;      // one pass, forward: threads per SM (64 registers each)
 constexpr int kMaxGroupChannels = 8192;     // (their sums stand in shared memory)
 constexpr int kMaxSpanGroups = 64;          // groups of a span
 
@@ -170,6 +170,19 @@ __device__ __forceinline__ void activate(float (&z)[E], bool relu)
     } else if (relu) {
 #pragma unroll
         for (int j = 0; j < E; ++j) z[j] = fmaxf(z[j], 0.0f);
+    }
+}
+// y = act(z).  ReLU of 16-bit types takes two values at a time, behind their rounding, which keeps the sign.
+template <typename T, int E, bool SILU>
+__device__ __forceinline__ void store_activated(T* y, float (&z)[E], bool relu)
+{
+    if constexpr (!SILU && sizeof(T) == 2 && E == 8) {
+        uint4 r = Pack<T>::put(z);
+        if (relu) r = positive(r, T());
+        *reinterpret_cast<uint4*>(y) = r;
+    } else {
+        activate<SILU, E>(z, relu);
+        store<T, E>(y, z);
     }
 }
 // d = dy * act'(z)
@@ -456,27 +469,27 @@ __device__ __forceinline__ void fetch_async(void* to, const void* from)
     else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(B) : "memory");
 }
 // The thread's n loads, `step` elements apart, on their way to its slots.
-template <typename T, int E>
+template <typename T, int E, int N>
 __device__ __forceinline__ void fetch(raw_t<T, E>* slot, const T* x, size_t step, int n)
 {
 #pragma unroll 4
     for (int i = 0; i < n; ++i, x += step) {
-        if constexpr (E * sizeof(T) >= 4) fetch_async<E * (int)sizeof(T)>(slot + i * kThreads, x);
-        else slot[i * kThreads] = load<T, E>(x);
+        if constexpr (E * sizeof(T) >= 4) fetch_async<E * (int)sizeof(T)>(slot + i * N, x);
+        else slot[i * N] = load<T, E>(x);
     }
 }
 __device__ __forceinline__ void fetched() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 __device__ __forceinline__ int pixels_of(const Args& a, int k) { return max(0, min(a.hw, (k + 1) * a.chunk) - k * a.chunk); }      // of block k of a cluster
 
-template <typename T, int E, bool SILU>
-__global__ void __launch_bounds__(kThreads, 8) norm_kernel(const Args a)
+template <typename T, int E, bool SILU, int N>
+__global__ void __launch_bounds__(N, kMostThreads / N) norm_kernel(const Args a)
 {
     extern __shared__ __align__(16) float red[];      // 2 E floats per thread; per channel; slots
-    __shared__ float count[kThreads];
+    __shared__ float count[N];
     __shared__ float2 own[kMaxSpanGroups];             // of the block's pixels: mean, squared distances from it
-    const Place<E, kThreads> at(a);
-    float* const mean = red + 2 * E * kThreads;        // of the image, per channel
+    const Place<E, N> at(a);
+    float* const mean = red + 2 * E * N;        // of the image, per channel
     float* const scale = mean + a.span_ch;             // rstd * gamma, beta
     float* const shift = scale + a.span_ch;
     raw_t<T, E>* const slot = reinterpret_cast<raw_t<T, E>*>(shift + a.span_ch) + threadIdx.x;
@@ -485,8 +498,8 @@ __global__ void __launch_bounds__(kThreads, 8) norm_kernel(const Args a)
     wait_for_previous();
     const size_t first = ((size_t)at.img * a.hw + at.p0 + at.r) * a.c + at.ch0 + ch, step = (size_t)at.rows * a.c;
     const int n = at.loads;
-    fetch<T, E>(slot, static_cast<const T*>(a.x) + first, step, n);
-    for (int i = threadIdx.x; i < at.nch; i += kThreads) {
+    fetch<T, E, N>(slot, static_cast<const T*>(a.x) + first, step, n);
+    for (int i = threadIdx.x; i < at.nch; i += N) {
         scale[i] = a.gamma ? __ldg(a.gamma + at.ch0 + i) : 1.0f;
         shift[i] = a.beta ? __ldg(a.beta + at.ch0 + i) : 0.0f;
     }
@@ -495,16 +508,16 @@ __global__ void __launch_bounds__(kThreads, 8) norm_kernel(const Args a)
 #pragma unroll 4
     for (int i = 0; i < n; ++i) {
         float v[E];
-        get<T, E>(slot[i * kThreads], v);
+        get<T, E>(slot[i * N], v);
         stat.take(v);
     }
-    unite<kThreads, E>(at, a, stat.n, stat.m, stat.q, red, count, own);
+    unite<N, E>(at, a, stat.n, stat.m, stat.q, red, count, own);
     if (a.chunks > 1) cluster_sync();
     else __syncthreads();
     // Every block unites the cluster's, a lane per (group, block), and spreads a group's result over its channels.
     const float total = 1.0f / ((float)a.hw * a.cg);
     const int lane = threadIdx.x & 31;
-    for (int i = threadIdx.x; i - lane < at.ng * a.chunks; i += kThreads) {
+    for (int i = threadIdx.x; i - lane < at.ng * a.chunks; i += N) {
         const int g = min(over(i, a.chdiv), at.ng - 1), r = i & (a.chunks - 1);      // (chunks: a power of two, at most 16)
         const float w = (float)pixels_of(a, r) * a.cg;
         const float2 o = a.chunks > 1 ? ld_rank(own + g, r) : own[g];
@@ -535,11 +548,10 @@ __global__ void __launch_bounds__(kThreads, 8) norm_kernel(const Args a)
 #pragma unroll 2
         for (int i = 0; i < n; ++i, y += step) {
             float v[E];
-            get<T, E>(slot[i * kThreads], v);
+            get<T, E>(slot[i * N], v);
             sub<E>(v, v, m);
             fma<E>(v, v, s, b);
-            activate<SILU, E>(v, a.relu);
-            store<T, E>(y, v);
+            store_activated<T, E, SILU>(y, v, a.relu);
         }
     }
     __syncwarp();
@@ -568,8 +580,8 @@ __global__ void __launch_bounds__(kThreads, 6) norm_back_kernel(const Args a)
     wait_for_previous();
     const size_t first = ((size_t)at.img * a.hw + at.p0 + at.r) * a.c + at.ch0 + ch, step = (size_t)at.rows * a.c;
     const int n = at.loads;
-    fetch<T, E>(slot, static_cast<const T*>(a.x) + first, step, n);
-    fetch<T, E>(dslot, static_cast<const T*>(a.dy) + first, step, n);
+    fetch<T, E, kThreads>(slot, static_cast<const T*>(a.x) + first, step, n);
+    fetch<T, E, kThreads>(dslot, static_cast<const T*>(a.dy) + first, step, n);
     for (int i = threadIdx.x; i < at.nch; i += kThreads) {
         const size_t g = (size_t)at.img * a.groups + at.span * a.gs + over(i, a.cdiv);
         mean[i] = a.mean[g];
@@ -808,8 +820,7 @@ __global__ void __launch_bounds__(kSplitThreads, 4) apply_kernel(const Args a)
                     get<T, E>(col.at(j), f);
                     sub<E>(f, f, m);
                     fma<E>(f, f, r, b);
-                    activate<SILU, E>(f, a.relu);
-                    store<T, E>(y, f);
+                    store_activated<T, E, SILU>(y, f, a.relu);
                     y += step;
                     col.ask(j, i + j + kDeep < loads);
                     asked();
@@ -1005,6 +1016,7 @@ __global__ void __launch_bounds__(1024) params_kernel(const float* sums, float* 
 struct NormPlan {
     int e;                     // elements per load
     int gs, chunk, loads;
+    int threads;               // of a block
     int cluster;               // one pass: blocks of a cluster; 0: two passes
     int chunks;                // blocks per (span, image)
     size_t smem, ring;         // shared memory of the (first) kernel; two passes: of the second
@@ -1012,43 +1024,70 @@ struct NormPlan {
 
 int gcd(int a, int b) { return b ? gcd(b, a % b) : a; }
 
+// One pass with blocks of `threads`: the span and cluster of the smallest estimate, in microseconds.  A block's loads and sums take an SM's issue slots (the more
+// warps are there, the better they are filled), but no less than their latencies; memory is idle meanwhile as far as all blocks are at the same; spans that
+// are parts of sectors cost memory time.  Fitted to sweeps of six shapes, from 4x14x14x512 (8 to 12 us) to 32x112x112x64 (55 to 75): within 15 % of the
+// best of each.
+struct OnePass {
+    NormPlan plan;
+    int resident;              // blocks an SM has room for
+    double per_sm;             // blocks of the call per SM
+    double us = 0;             // 0: no span fits
+};
+OnePass one_pass(int threads, NormPlan p, int n, int hw, int c, int groups, int gs0, int elt, bool back, bool silu, int sms)
+{
+    OnePass best = {};
+    const int cg = c / groups;
+    p.threads = threads;
+    for (int gs = gs0;; gs *= 2) {
+        const long long nv = (long long)gs * cg / p.e, nch = up_div((long long)gs * cg, 4) * 4;
+        if (gs > kMaxSpanGroups || gs > std::max(gs0, groups) || nv > kThreads) break;
+        const int rows = (int)(threads / nv), bytes = gs * cg * elt;
+        for (int cluster = 1; cluster <= kMaxCluster; cluster *= 2) {
+            const int chunk = (int)up_div(hw, cluster), loads = (int)up_div(chunk, rows);
+            if (cluster > 1 && up_div(hw, chunk) <= cluster / 2) break;
+            const int slots = !back ? 1 : silu && elt == 2 ? 3 : 2;
+            const size_t smem = (size_t)threads * p.e * 8 + (back ? 6 : 3) * nch * 4 + (size_t)loads * slots * threads * p.e * elt;
+            if (smem > 200 * 1024) continue;
+            const int resident = std::min<int>(back ? 6 : kMostThreads / threads, (int)(225 * 1024 / (smem + 1024)));
+            const double per_sm = (double)n * up_div(groups, gs) * cluster / sms, at_once = std::min((double)resident, std::max(1.0, per_sm));
+            const double per_load = 0.015 + p.e * (back ? (silu ? 0.017 : 0.010) : silu ? 0.0085 : 0.0065);
+            const double latency = 2.5 + 0.1 * loads + (cluster > 1 ? 1.5 : 0) + (cluster > 8 ? 1.5 : 0);
+            const double times = (double)threads / kThreads, warps = at_once * times;      // (in units of kThreads)
+            const double slots_time = per_sm * (1 + loads * per_load) * times * (warps >= 6 ? 1 : warps >= 4 ? 1.15 : 1.4);
+            const double memory = (double)n * hw * c * elt * (back ? 3 : 2) / 6.2e6 * (bytes >= 64 ? 1 : bytes >= 32 ? 1.25 : 2) * (per_sm > 2 * at_once ? 0.6 : 1);
+            const double us = std::max(slots_time, std::ceil(per_sm / at_once) * latency) + memory;
+            if (best.us == 0 || us < best.us) {
+                p.gs = gs; p.cluster = p.chunks = cluster; p.chunk = chunk; p.loads = loads; p.smem = smem;
+                best = {p, resident, per_sm, us};
+            }
+        }
+    }
+    return best;
+}
+
 NormPlan make_plan(int n, int hw, int c, int groups, int elt, int align, bool back, bool silu, int sms)
 {
     NormPlan p = {};
     const int cg = c / groups;
     for (p.e = 16 / elt; p.e > 1 && (c % p.e || align % (p.e * elt)); p.e /= 2) {}      // elements of a load
     int gs0 = p.e / gcd(p.e, cg);                       // groups whose channels are whole loads
-    // One pass: the spans and clusters of the smallest estimate, in microseconds.  A block's loads and sums take an SM's issue slots (the more blocks are there,
-    // the better they are filled), but no less than their latencies; memory is idle meanwhile as far as all blocks are at the same; spans that are parts of
-    // sectors cost memory time.  Fitted to sweeps of six shapes, from 4x14x14x512 (8 to 12 us) to 32x112x112x64 (55 to 75): within 15 % of the best of each.
-    double best = 0;
     // The backward pass holds x, dy and, with SiLU, dz: few blocks per SM.  Large calls, which keep the memory busy either way, are faster in two passes
     // (64 images of 56x56x256, SiLU: 162 us in one pass, 106 in two; 32 of 28x28x256: 18 and 25).
-    for (int gs = gs0; !back || (long long)n * hw * c * elt <= (32 << 20); gs *= 2) {
-        const long long nv = (long long)gs * cg / p.e, nch = up_div((long long)gs * cg, 4) * 4;
-        if (gs > kMaxSpanGroups || gs > std::max(gs0, groups) || nv > kThreads) break;
-        const int rows = (int)(kThreads / nv), bytes = gs * cg * elt;
-        for (int cluster = 1; cluster <= kMaxCluster; cluster *= 2) {
-            const int chunk = (int)up_div(hw, cluster), loads = (int)up_div(chunk, rows);
-            if (cluster > 1 && up_div(hw, chunk) <= cluster / 2) break;
-            const int slots = !back ? 1 : silu && elt == 2 ? 3 : 2;
-            const size_t smem = (size_t)kThreads * p.e * 8 + (back ? 6 : 3) * nch * 4 + (size_t)loads * slots * kThreads * p.e * elt;
-            if (smem > 200 * 1024) continue;
-            const int resident = std::min<int>(back ? 6 : 8, (int)(225 * 1024 / (smem + 1024)));
-            const double per_sm = (double)n * up_div(groups, gs) * cluster / sms, at_once = std::min((double)resident, std::max(1.0, per_sm));
-            const double per_load = 0.015 + p.e * (back ? (silu ? 0.017 : 0.010) : silu ? 0.0085 : 0.0065);
-            const double latency = 2.5 + 0.1 * loads + (cluster > 1 ? 1.5 : 0) + (cluster > 8 ? 1.5 : 0);
-            const double slots_time = per_sm * (1 + loads * per_load) * (at_once >= 6 ? 1 : at_once >= 4 ? 1.15 : 1.4);
-            const double memory = (double)n * hw * c * elt * (back ? 3 : 2) / 6.2e6 * (bytes >= 64 ? 1 : bytes >= 32 ? 1.25 : 2) * (per_sm > 2 * at_once ? 0.6 : 1);
-            const double us = std::max(slots_time, std::ceil(per_sm / at_once) * latency) + memory;
-            if (best == 0 || us < best) {
-                best = us;
-                p.gs = gs; p.cluster = p.chunks = cluster; p.chunk = chunk; p.loads = loads; p.smem = smem;
-            }
+    if (!back || (long long)n * hw * c * elt <= (32 << 20)) {
+        const OnePass one = one_pass(kThreads, p, n, hw, c, groups, gs0, elt, back, silu, sms);
+        // Blocks of twice the threads have the same shared memory and more warps: where an SM has room for three blocks or fewer and there are several rounds of
+        // them (64x56x56x256 bf16 with SiLU: 66 us, so 58; 128x28x28x512: 59 and 51; 64x28x28x256 fp32: 29 and 24), or not a block for every SM
+        // (1x224x224x64: 20 and 12).  With more blocks per SM, or one round, their sums cost more than that gives (16x56x56x256 fp32: 27 and 29;
+        // 16x112x112x64 bf16: 20 and 24).
+        if (one.us > 0 && !back && ((one.resident <= 3 && one.per_sm > 2 * one.resident) || (one.per_sm <= 1 && one.plan.loads > 16))) {
+            const OnePass two = one_pass(2 * kThreads, p, n, hw, c, groups, gs0, elt, back, silu, sms);
+            if (two.us > 0) return two.plan;
         }
+        if (one.us > 0) return one.plan;
     }
-    if (best > 0) return p;
     // Two passes.  A span of more loads than threads has to be one group.
+    p.threads = kSplitThreads;
     if ((long long)gs0 * cg / p.e > kSplitThreads && gs0 > 1) { p.e = 1; gs0 = 1; }
     p.gs = gs0;
     while (p.gs * 2 <= std::min(kMaxSpanGroups, groups) && (long long)p.gs * 2 * cg / p.e <= kSplitThreads) p.gs *= 2;
@@ -1087,28 +1126,29 @@ int check_shape(int n, int h, int wd, int c, int groups)
 using Kernel = void (*)(const Args);
 // which: 0 one pass, 1 statistics, 2 outputs
 template <typename T, int E>
-Kernel kernel_of(bool back, int which, bool silu)
+Kernel kernel_of(bool back, int which, bool silu, int threads)
 {
-    if (which == 0) return back ? (silu ? norm_back_kernel<T, E, true> : norm_back_kernel<T, E, false>) : silu ? norm_kernel<T, E, true> : norm_kernel<T, E, false>;
+    if (which == 0 && !back && threads > kThreads) return silu ? norm_kernel<T, E, true, 2 * kThreads> : norm_kernel<T, E, false, 2 * kThreads>;
+    if (which == 0) return back ? (silu ? norm_back_kernel<T, E, true> : norm_back_kernel<T, E, false>) : silu ? norm_kernel<T, E, true, kThreads> : norm_kernel<T, E, false, kThreads>;
     if (which == 1) return back ? (silu ? back_stats_kernel<T, E, true> : back_stats_kernel<T, E, false>) : stats_kernel<T, E>;
     return back ? (silu ? back_apply_kernel<T, E, true> : back_apply_kernel<T, E, false>) : silu ? apply_kernel<T, E, true> : apply_kernel<T, E, false>;
 }
 template <typename T>
-Kernel kernel_of(int e, bool back, int which, bool silu)
+Kernel kernel_of(int e, bool back, int which, bool silu, int threads)
 {
-    if (e == 1) return kernel_of<T, 1>(back, which, silu);
-    if (e == 2) return kernel_of<T, 2>(back, which, silu);
+    if (e == 1) return kernel_of<T, 1>(back, which, silu, threads);
+    if (e == 2) return kernel_of<T, 2>(back, which, silu, threads);
     if constexpr (sizeof(T) == 2) {
-        if (e == 4) return kernel_of<T, 4>(back, which, silu);
-        return kernel_of<T, 8>(back, which, silu);
+        if (e == 4) return kernel_of<T, 4>(back, which, silu, threads);
+        return kernel_of<T, 8>(back, which, silu, threads);
     } else {
-        return kernel_of<T, 4>(back, which, silu);
+        return kernel_of<T, 4>(back, which, silu, threads);
     }
 }
 Kernel kernel_of(alcs_dtype dt, const NormPlan& p, bool back, int which, bool silu)
 {
-    return dt == ALCS_F32 ? kernel_of<float>(p.e, back, which, silu) : dt == ALCS_F16 ? kernel_of<__half>(p.e, back, which, silu)
-                                                                                        : kernel_of<__nv_bfloat16>(p.e, back, which, silu);
+    return dt == ALCS_F32 ? kernel_of<float>(p.e, back, which, silu, p.threads) : dt == ALCS_F16 ? kernel_of<__half>(p.e, back, which, silu, p.threads)
+                                                                                        : kernel_of<__nv_bfloat16>(p.e, back, which, silu, p.threads);
 }
 
 int align_of(std::initializer_list<const void*> ps)
@@ -1155,12 +1195,12 @@ int run(Args& a, bool back, alcs_dtype dt, int dev, const NormPlan& p, void* wor
     a.spdiv = tc_div(a.spans);
     const int nv = a.gs * a.cg / p.e;
     a.nvdiv = tc_div(nv);
-    a.rowdiv = tc_div(std::max(1, (p.cluster ? kThreads : kSplitThreads) / nv));
+    a.rowdiv = tc_div(std::max(1, p.threads / nv));
     const dim3 grid((unsigned)blocks);
     const Kernel first = kernel_of(dt, p, back, p.cluster ? 0 : 1, a.silu);
     const int rc = allow((const void*)first, p.smem, p.cluster, dev);
     if (rc) return rc;
-    ALCS_CUDA(launch_pdl(first, grid, p.cluster ? kThreads : kSplitThreads, p.smem, std::max(1, p.cluster), st, a));
+    ALCS_CUDA(launch_pdl(first, grid, p.threads, p.smem, std::max(1, p.cluster), st, a));
     if (p.cluster) return ALCS_OK;
     if (back && (a.dgamma || a.dbeta)) a.first = (int)up_div(a.c, 8);
     if (blocks + a.first > 0x7fffffffll) return ALCS_ERR_SHAPE;
