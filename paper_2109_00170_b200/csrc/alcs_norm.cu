@@ -10,7 +10,7 @@
 // of a pixel where that is possible: whole sectors of memory) of one image; its pixels are shared out to the blocks of a cluster, and a block holds its
 // share in shared memory, which cp.async fills without holding registers.  A thread keeps to its channels.  Sums go through shared memory, in a fixed
 // order, and between the cluster's blocks through distributed shared memory.  What it costs over a copy is the sums: all blocks of an SM tend to be at them
-// at the same time, with memory idle (64 images of 56x56x128, bf16: 29.5 us among other calls; a copy of them 22.5; the same
+// at the same time, with memory idle (64 images of 56x56x128, bf16: 29.4 us among other calls; a copy of them 22.5; the same
 // kernel without the sums 24.6; floor 15.7 at 6.5 TB/s).
 //
 // Two passes: sums of chunks of pixels, then the outputs from a second reading, which L2 serves as far as it holds x (and dy).  For spans that do

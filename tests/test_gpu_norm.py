@@ -130,6 +130,14 @@ def test_large_calls(alcs, case):
     assert (k.forward() == y).all() and (k.backward(dy) == dx).all()
 
 
+# Several rounds of blocks that an SM has room for few of, and fewer blocks than SMs: twice the threads; loads of 16, 8 and 4 bytes, groups that are not whole loads
+@pytest.mark.parametrize("case", [(1, 224, 224, 64, 32, "bf16", "silu"), (64, 28, 28, 256, 32, "f32", "relu"), (20, 112, 112, 120, 30, "bf16", "relu"),
+                                  (1, 224, 221, 66, 22, "f16", "none"), (70, 28, 27, 250, 25, "f32", "silu"), (128, 28, 28, 160, 20, "f16", "silu")],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_blocks_of_twice_the_threads(alcs, case):
+    test_large_calls(alcs, case)
+
+
 @pytest.mark.parametrize("shape", [(2, 14, 14, 128, 8), (1, 130, 120, 64, 2)])
 def test_without_parameters_and_statistics(alcs, shape):
     n, h, w, c, groups = shape
