@@ -521,7 +521,7 @@ __global__ void __launch_bounds__(N, kMostThreads / N) norm_kernel(const Args a)
         const int g = min(over(i, a.chdiv), at.ng - 1), r = i & (a.chunks - 1);      // (chunks: a power of two, at most 16)
         const float w = (float)pixels_of(a, r) * a.cg;
         const float2 o = a.chunks > 1 ? ld_rank(own + g, r) : own[g];
-        const float mu = w > 0.0f ? lanes_sum(o.x * w, a.chunks) * total : lanes_sum(0.0f, a.chunks) * total;
+        const float mu = lanes_sum(w > 0.0f ? o.x * w : 0.0f, a.chunks) * total;      // (a block without pixels adds nothing, but its lanes take part)
         const float d = o.x - mu;
         const float var = lanes_sum(w > 0.0f ? fmaf(d * d, w * total, o.y * total) : 0.0f, a.chunks);      // (each part's share: less than their sum)
         const float rs = 1.0f / sqrtf(var + a.eps);
