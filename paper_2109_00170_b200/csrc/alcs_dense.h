@@ -161,7 +161,8 @@ __device__ __forceinline__ void fma(float (&d)[E], const float (&a)[E], const fl
             asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
                 : "=f"(d[i]), "=f"(d[i + 1]) : "f"(a[i]), "f"(a[i + 1]), "f"(b[i]), "f"(b[i + 1]), "f"(c[i]), "f"(c[i + 1]));
 }
-// Programmatic dependent launch: the next kernel on the stream may set up, this one waits for what the one before it wrote.
+// Programmatic dependent launch: the next kernel on the stream may set up, this one waits for what the one before it wrote.  A kernel thus runs while its
+// inputs, parameters too, may still be written: it reads them by ordinary loads behind the wait.  The read-only path wants memory that nobody writes during the kernel.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

@@ -62,7 +62,7 @@ __device__ __forceinline__ void load8(const T* row, int c, int cols, Eight<T>& v
         for (int i = 0; i < 8 / n; ++i) {
             v.r[i] = make_uint4(0, 0, 0, 0);
             if (c + i * n < cols)
-                asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.r[i].x), "=r"(v.r[i].y), "=r"(v.r[i].z), "=r"(v.r[i].w) : "l"(row + c + i * n));
+                asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.r[i].x), "=r"(v.r[i].y), "=r"(v.r[i].z), "=r"(v.r[i].w) : "l"(row + c + i * n));
         }
     } else {
         T* const e = reinterpret_cast<T*>(&v);
@@ -149,10 +149,10 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const Args a)
         const int band = band_of(a, u), quad = (int)(u - (long long)band * a.quads.d), r = band * 8 + (lane >> 2);
         if (r >= a.rows) continue;
         const unsigned char* from = a.data + ((size_t)(r >> 7) * a.blocks + quad * 4) * 2048 + (r & 127) * 16 + q * 4;
-        const unsigned scales = __ldg(reinterpret_cast<const unsigned*>(a.scales + ((size_t)(r >> 7) * a.quads.d + quad) * 512 + (r & 31) * 16 + (r >> 5 & 3) * 4));
+        const unsigned scales = *reinterpret_cast<const unsigned*>(a.scales + ((size_t)(r >> 7) * a.quads.d + quad) * 512 + (r & 31) * 16 + (r >> 5 & 3) * 4);
         unsigned code[4];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) code[b] = quad * 4 + b < a.blocks ? __ldg(reinterpret_cast<const unsigned*>(from + b * 2048)) : 0u;
+        for (int b = 0; b < 4; ++b) code[b] = quad * 4 + b < a.blocks ? *reinterpret_cast<const unsigned*>(from + b * 2048) : 0u;
         T* row = static_cast<T*>(a.y) + (size_t)r * a.ld;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {

@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
 #pragma unroll 1
             for (unsigned h = 0; h < halves && ok; ++h) {
                 const int c0 = tb * n + (int)h * kSlotCols + part_of * 32, end = min(tb * n + n, a.b.rows);
-                const float bias = a.bias && a.split == 1 && c0 + lane < end ? __ldg(a.bias + c0 + lane) : 0.0f;      // of the lane's column
+                const float bias = a.bias && a.split == 1 && c0 + lane < end ? a.bias[c0 + lane] : 0.0f;      // of the lane's column
                 float v[32];
                 ok = __all_sync(0xffffffffu, bar_wait(acc_full + 8 * acc, acc_ph));
                 if (!ok) break;
@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
             const int ga = ta * 128 + row, gb = tb * n + col;
             if (ga >= a.a.rows || gb >= a.b.rows) continue;
             const int c = a.swapped ? ga : gb, p = a.swapped ? gb : ga;
-            store_one<T>(a, (size_t)p * a.cout + c, sum, a.bias ? __ldg(a.bias + c) : 0.0f);
+            store_one<T>(a, (size_t)p * a.cout + c, sum, a.bias ? a.bias[c] : 0.0f);
         }
         __syncwarp();
         cluster_arrive();

@@ -500,8 +500,8 @@ __global__ void __launch_bounds__(N, kMostThreads / N) norm_kernel(const Args a)
     const int n = at.loads;
     fetch<T, E, N>(slot, static_cast<const T*>(a.x) + first, step, n);
     for (int i = threadIdx.x; i < at.nch; i += N) {
-        scale[i] = a.gamma ? __ldg(a.gamma + at.ch0 + i) : 1.0f;
-        shift[i] = a.beta ? __ldg(a.beta + at.ch0 + i) : 0.0f;
+        scale[i] = a.gamma ? a.gamma[at.ch0 + i] : 1.0f;
+        shift[i] = a.beta ? a.beta[at.ch0 + i] : 0.0f;
     }
     fetched();
     Running<E> stat;
@@ -586,8 +586,8 @@ __global__ void __launch_bounds__(kThreads, 6) norm_back_kernel(const Args a)
         const size_t g = (size_t)at.img * a.groups + at.span * a.gs + over(i, a.cdiv);
         mean[i] = a.mean[g];
         rstd[i] = a.rstd[g];
-        gamma[i] = a.gamma ? __ldg(a.gamma + at.ch0 + i) : 1.0f;
-        beta[i] = a.beta ? __ldg(a.beta + at.ch0 + i) : 0.0f;
+        gamma[i] = a.gamma ? a.gamma[at.ch0 + i] : 1.0f;
+        beta[i] = a.beta ? a.beta[at.ch0 + i] : 0.0f;
     }
     __syncthreads();
     float m[E], g[E], b[E], u[E], w[E];
@@ -675,8 +675,8 @@ __device__ __forceinline__ void channels(const Args& a, int ch0, int ch, const f
         if (j == next) { ++q; next += a.cg; }
         m[j] = mean[q];
         r[j] = rstd[q];
-        g[j] = a.gamma ? __ldg(a.gamma + ch0 + ch + j) : 1.0f;
-        b[j] = a.beta ? __ldg(a.beta + ch0 + ch + j) : 0.0f;
+        g[j] = a.gamma ? a.gamma[ch0 + ch + j] : 1.0f;
+        b[j] = a.beta ? a.beta[ch0 + ch + j] : 0.0f;
     }
 }
 
@@ -843,7 +843,7 @@ __global__ void __launch_bounds__(kSplitThreads, 3) back_stats_kernel(const Args
     wait_for_previous();
     const size_t q0 = (size_t)at.img * a.groups + at.span * a.gs;
     for (int i = threadIdx.x; i < at.nch; i += kSplitThreads) {
-        gamma[i] = a.gamma ? __ldg(a.gamma + at.ch0 + i) : 1.0f;
+        gamma[i] = a.gamma ? a.gamma[at.ch0 + i] : 1.0f;
         rstd[i] = a.rstd[q0 + over(i, a.cdiv)];
     }
     float u[E], w[E];
