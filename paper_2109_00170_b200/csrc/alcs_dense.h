@@ -165,6 +165,17 @@ __device__ __forceinline__ void fma(float (&d)[E], const float (&a)[E], const fl
 // inputs, parameters too, may still be written: it reads them by ordinary loads behind the wait.  The read-only path wants memory that nobody writes during the kernel.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The two halves of a barrier of the cluster's blocks.  A warp's lanes have to come to an .aligned instruction together, whatever branch they were in before.
+__device__ __forceinline__ void cluster_arrive()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 
 template <typename... P, typename... A>
 cudaError_t launch_pdl(void (*fn)(P...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st, const A&... a)

@@ -75,8 +75,6 @@ __device__ __forceinline__ void scales_to_tmem(unsigned d, unsigned at)
 }
 // The address field of a matrix descriptor: 14 bits (in a cluster an address carries the block's rank above them).
 __device__ __forceinline__ unsigned field(unsigned addr) { return addr >> 4 & 0x3fffu; }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ unsigned cluster_rank()
 {
     unsigned r;
@@ -372,7 +370,6 @@ __global__ void __launch_bounds__(kThreads, 1) mx4_kernel(const Args a)
             const int c = a.swapped ? ga : gb, p = a.swapped ? gb : ga;
             store_one<T>(a, (size_t)p * a.cout + c, sum, a.bias ? a.bias[c] : 0.0f);
         }
-        __syncwarp();
         cluster_arrive();
         cluster_wait();
     }

@@ -205,7 +205,8 @@ __device__ __forceinline__ void activate_back(float (&d)[E], float (&z)[E], bool
 
 __device__ __forceinline__ void cluster_sync()
 {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    cluster_arrive();
+    cluster_wait();
 }
 __device__ __forceinline__ float2 ld_rank(const float2* p, int rank)      // the same place in another block's shared memory
 {
@@ -538,7 +539,7 @@ __global__ void __launch_bounds__(N, kMostThreads / N) norm_kernel(const Args a)
         }
     }
     __syncthreads();
-    if (a.chunks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // done with the others' shared memory
+    if (a.chunks > 1) cluster_arrive();      // done with the others' shared memory
     if (n) {
         T* y = static_cast<T*>(a.out) + first;
         float m[E], s[E], b[E];
@@ -554,8 +555,7 @@ __global__ void __launch_bounds__(N, kMostThreads / N) norm_kernel(const Args a)
             store_activated<T, E, SILU>(y, v, a.relu);
         }
     }
-    __syncwarp();
-    if (a.chunks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (a.chunks > 1) cluster_wait();
 }
 
 // With SiLU, dz of the first pass is kept for the second, in the place of dy (and, of 16 bits, in as much again): to compute it again would
@@ -632,7 +632,7 @@ __global__ void __launch_bounds__(kThreads, 6) norm_back_kernel(const Args a)
             for (int j = k; j < a.cg; j += a.chunks) { red[q * a.cg + j] = s1; red[at.nch + q * a.cg + j] = s2; }
     }
     __syncthreads();
-    if (a.chunks > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    if (a.chunks > 1) cluster_arrive();
     if (n) {      // dx = (rstd gamma) dz - rstd k1 - (rstd^2 k2) (x - mean)
         T* dx = static_cast<T*>(a.out) + first;
         load_shared<E>(u, red + ch);
@@ -657,8 +657,7 @@ __global__ void __launch_bounds__(kThreads, 6) norm_back_kernel(const Args a)
             store<T, E>(dx, v);
         }
     }
-    __syncwarp();
-    if (a.chunks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (a.chunks > 1) cluster_wait();
 }
 
 // ---------------------------------------------------------------------------------------------
