@@ -132,9 +132,11 @@ __device__ __forceinline__ void store_shared(float* p, const float (&d)[E])
 }
 
 // s = 1 / (1 + exp(-z)).  What bounds SiLU is the special function unit: two neighbours share a reciprocal (r = 1 / (a b), 1 / a = r b), so that an
-// element takes it one and a half times.  exp(-z) stays below 2^62 for that, so s is not below 2^-62.  Each instruction is good to 2^-22 or so.
+// element takes it one and a half times.  exp(-z) is held below 2^62 for that, and z, whose product with s is wanted, above -43, where that is: SiLU and its slope stay
+// what they are there, -9.3e-18, however low z is (1 to 2 % of a SiLU pass; an exact branch for what lies below cost 3 to 10).  Each instruction is good to 2^-22
+// or so, and the exponent to z 2^-24.
 template <int E>
-__device__ __forceinline__ void sigmoid(float (&s)[E], const float (&z)[E])
+__device__ __forceinline__ void sigmoid(float (&s)[E], float (&z)[E])
 {
     float k[E], one[E];
     set<E>(k, -1.4426950408889634f);
@@ -144,6 +146,7 @@ __device__ __forceinline__ void sigmoid(float (&s)[E], const float (&z)[E])
     for (int j = 0; j < E; ++j) {
         s[j] = fminf(s[j], 62.0f);      // (NaN, too, which its own z brings back, so that a neighbour's stays its own)
         asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(s[j]));
+        asm("max.NaN.f32 %0, %0, %1;" : "+f"(z[j]) : "f"(-43.0f));      // (a NaN stays)
     }
     add<E>(s, s, one);
     if constexpr (E == 1) {

@@ -1,7 +1,10 @@
-"""Group norm at the edges of its ranges: clusters with blocks that have no pixels; chains of calls through the same buffers."""
+"""Group norm at the edges of its ranges: clusters with blocks that have no pixels; chains of calls through the same buffers; SiLU far below 0."""
+import numpy as np
 import pytest
 
 import test_gpu_norm as norm
+from dense_util import D, HALF, TINY, U, back_bounds, f64, norm_bound
+from oracle import dense
 
 pytestmark = pytest.mark.gpu
 
@@ -57,3 +60,52 @@ def test_a_chain_whose_buffers_are_used_again(alcs):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(values, want[0]) and torch.equal(ys, want[1])
+
+
+# loads of 8, 2 and 1 elements; a group that is not whole loads; two passes
+@pytest.mark.parametrize("shape", [(2, 9, 9, 96, 12), (3, 7, 5, 150, 30), (2, 11, 9, 35, 5), (3, 13, 11, 66, 22), (1, 448, 448, 32, 8), (70, 56, 56, 64, 8)],
+                         ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_silu_far_below_zero(alcs, shape, dtype):
+    """Group 0 has a beta of -30 to -105, group 1 the lowest number, group 2 minus infinity (a channel that is masked out).
+
+    y: a relative error is what z is off by, q = D u |gamma| (|xh| + M) + 2 u |z| with M = max|x| rstd, as in norm_bound, and (8 + 2 |z|) u of exp and the
+    quotient; below -43 y stays what it is there, 43 x 2^-62 = 9.33e-18 and less than 1e-17 with that error, instead of going to 0.  The slope s + z s (1 - s) is
+    between z exp(z) and half of it there, so that it is off by twice the relative error, and by less than 1e-17 below -43.  dx: every term is off by that of dz and by 2 D u (1 + M)
+    of xh, rstd and the sums, as in back_bounds."""
+    import torch
+    n, h, w, c, groups = shape
+    x, dy, gamma, beta = norm._inputs(sum(shape), n, h * w, c, dtype, alcs)
+    k, far = c // groups, 1e-17
+    beta[:k] = -torch.linspace(30, 105, k, device="cuda")
+    beta[k:2 * k], beta[2 * k:3 * k] = float(np.finfo(np.float32).min), float("-inf")
+    call = norm.Norm(alcs, x, shape, dtype, "silu", 1e-5, gamma, beta)
+    y, dx = f64(call.forward()), f64(call.backward(dy))
+    dgamma, dbeta = f64(call.dgamma), f64(call.dbeta)
+    # the other groups are what they are
+    rest = slice(3 * k, c)
+    args = f64(x[..., rest]), f64(gamma[rest]), f64(beta[rest])
+    ref = dense.group_norm_backward(args[0], f64(dy[..., rest]), groups - 3, *args[1:], 1e-5, "silu")
+    assert (np.abs(y[..., rest] - ref["y"]) <= norm_bound(ref, *args, groups - 3, dtype)).all()
+    assert (np.abs(dx[..., rest] - ref["dx"]) <= back_bounds(ref, args[0], f64(dy[..., rest]), *args[1:], groups - 3, dtype)[0]).all()
+    for g in range(3):
+        at = slice(g * k, (g + 1) * k)
+        xg, dyg, gg = f64(x[..., at]), f64(dy[..., at]), np.abs(f64(gamma[at]))
+        ref = dense.group_norm_backward(xg, dyg, 1, f64(gamma[at]), f64(beta[at]) if g == 0 else None, 1e-5, "silu" if g == 0 else "none")
+        xh, r = np.abs(ref["xh"]), ref["rstd"][:, :, None]
+        m = np.abs(xg).max((1, 2), keepdims=True) * r
+        if g == 0:
+            z = np.abs(ref["z"])
+            q, want, dz, want_dx = D * U * gg * (xh + m) + U * (8 + 4 * z), ref["y"], dyg * dense.activation_slope(ref["z"], "silu"), ref["dx"]
+        else:      # masked out: z is -3e38 or minus infinity
+            q, want, dz, want_dx = 0 * xh, 0 * xh, 0 * xh, 0 * xh
+        bound = q * np.abs(want) + far
+        assert (np.abs(y[..., at] - want) <= bound + HALF[dtype] * (np.abs(want) + bound) + TINY[dtype]).all()
+        off = 2 * q.max() * np.abs(dz) + far * np.abs(dyg)      # of dz
+        e = 2 * D * U * (1 + m)
+        t, o = np.abs(gg * dz), gg * off
+        mean = lambda v: v.mean((1, 2), keepdims=True)  # noqa: E731
+        bound = r * (o + mean(o) + xh * mean(o * xh) + e * (t + mean(t) * (1 + xh) + (1 + xh) * mean(t * xh)))
+        assert (np.abs(dx[..., at] - want_dx) <= bound + HALF[dtype] * (np.abs(want_dx) + bound) + TINY[dtype]).all()
+        for got, f in ((dgamma[at], ref["xh"]), (dbeta[at], 1 + 0 * xh)):
+            assert (np.abs(got - (dz * f).sum((0, 1))) <= (off * np.abs(f) + e * np.abs(dz) * (1 + xh)).sum((0, 1))).all()
