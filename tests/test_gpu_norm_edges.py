@@ -1,4 +1,4 @@
-"""Group norm at the edges of its ranges: clusters with blocks that have no pixels; chains of calls through the same buffers; SiLU far below 0."""
+"""Group norm at the edges of its ranges: clusters with blocks that have no pixels; chains of calls through the same buffers; SiLU far below 0; the most channels."""
 import numpy as np
 import pytest
 
@@ -109,3 +109,10 @@ def test_silu_far_below_zero(alcs, shape, dtype):
         assert (np.abs(dx[..., at] - want_dx) <= bound + HALF[dtype] * (np.abs(want_dx) + bound) + TINY[dtype]).all()
         for got, f in ((dgamma[at], ref["xh"]), (dbeta[at], 1 + 0 * xh)):
             assert (np.abs(got - (dz * f).sum((0, 1))) <= (off * np.abs(f) + e * np.abs(dz) * (1 + xh)).sum((0, 1))).all()
+
+
+@pytest.mark.parametrize("shape", [(1, 2, 2, 65536, 8), (2, 1, 3, 65536, 65536), (1, 3, 3, 65528, 8), (1, 5, 5, 65535, 1285), (1, 12, 11, 65536, 1024)],
+                         ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype,act", [("f32", "none"), ("bf16", "silu")])
+def test_the_most_channels(alcs, shape, dtype, act):
+    norm.test_forward_and_backward(alcs, shape, dtype, act)
