@@ -459,7 +459,8 @@ ALCS_API int alcs_spconv2d_plan(const alcs_packed* w, int n, int cin, int h, int
  * overlap it otherwise.  gamma and beta are device fp32 [c] or NULL (1 and 0); mean and rstd receive mu and rstd, device fp32
  * [n][groups], or are NULL.  Statistics and everything up to the rounding of y are fp32; the variance comes from
  * running means and differences of means, so that a mean far from 0 costs no accuracy but its own rounding to fp32.  An infinity
- * or NaN in x makes its group of its image NaN.  ReLU turns NaN into 0, as in the convolutions.  SiLU and its slope for z below -43
+ * or NaN in x makes its group of its image NaN.  Distances from the mean whose squares are beyond fp32 (1.8e19 and more) give an rstd of 0, and so
+ * y = act(beta), dx = 0 and dgamma = 0; x is at most 2^126 in magnitude for that.  ReLU turns NaN into 0, as in the convolutions.  SiLU and its slope for z below -43
  * (a beta of -FLT_MAX or -infinity as a mask) are what they are at -43, -9.3e-18, instead of less.
  *
  * alcs_group_norm_backward: for the derivative dy of a loss by y, with dz = dy * act'(z) (act' of ReLU at 0 is 0) and t = gamma * dz,

@@ -19,7 +19,7 @@
 // 46 and 51 us for the passes now).
 //
 // The variance has no cancellation: a thread takes its values one by one into a running mean and sum of squared distances, and these are united by
-// M2 = M2_a + M2_b + n_a n_b / n (mean_a - mean_b)^2.  All of it in fp32.
+// M2 = M2_a + M2_b + n_a n_b / n (mean_a - mean_b)^2.  A mean of means is a sum of each one's share, so that no sum is larger than the values.  All of it in fp32.
 #include <algorithm>
 #include <cmath>
 #include <mutex>
@@ -336,15 +336,15 @@ struct Running {
 };
 
 // n values of mean m and sum of squared distances q, united with as many again as `other` says.  Either may be none (m = q = 0): the distance of the means then
-// is the size of a value, whose square may not be a number of fp32 (0 times which is NaN), and is multiplied by 0 before it is squared.
+// is the size of a value, whose square, or n times which, may not be a number of fp32 (0 times which is NaN), and is multiplied by 0 before it is squared.
 struct Union {
-    float n, to;      // to: share of the other's
-    __device__ __forceinline__ Union(float n_, float other) : n(n_), to(n + other > 0.0f ? other / (n + other) : 0.0f) {}
+    float to, w;      // share of the other's; weight of the squared distance of the means
+    __device__ __forceinline__ Union(float n, float other) : to(n + other > 0.0f ? other / (n + other) : 0.0f), w(n * to) {}
     __device__ __forceinline__ void operator()(float& m, float& q, float om, float oq) const
     {
         const float d = om - m;
         m = fmaf(d, to, m);
-        q += fmaf(d * to, d * n, oq);
+        q += fmaf(d * w, d, oq);
     }
 };
 
@@ -359,8 +359,7 @@ __device__ __forceinline__ void unite(const Place<E, N>& at, const Args& a, floa
     if (a.whole && E > 1) {      // the thread's channels are one group's
         float s = 0.0f, t = 0.0f;
 #pragma unroll
-        for (int j = 0; j < E; ++j) s += m[j];
-        s *= 1.0f / E;
+        for (int j = 0; j < E; ++j) s = fmaf(m[j], 1.0f / E, s);
 #pragma unroll
         for (int j = 0; j < E; ++j) t += fmaf((m[j] - s) * k, m[j] - s, q[j]);
         m[0] = s;
@@ -399,9 +398,9 @@ __device__ __forceinline__ void unite(const Place<E, N>& at, const Args& a, floa
         float s = 0.0f, t = 0.0f;
         for (int e = sub; e < rows * w; e += l) {
             const int r = over(e, a.whole ? a.vdiv : a.cdiv);
-            s = fmaf(from[r * per + e - r * w], count[r], s);
+            s = fmaf(from[r * per + e - r * w], count[r] * inv, s);
         }
-        s = lanes_sum(s, l) * inv;
+        s = lanes_sum(s, l);
         for (int e = sub; e < rows * w; e += l) {
             const int r = over(e, a.whole ? a.vdiv : a.cdiv), i = r * per + e - r * w;
             const float d = from[i] - s;
@@ -411,6 +410,9 @@ __device__ __forceinline__ void unite(const Place<E, N>& at, const Args& a, floa
         if (sub == 0 && g == g0) out[g] = make_float2(s, t);
     }
 }
+
+// rstd times a sum of dz (x - mean): 0 where rstd is, even if the distances that it is 0 for have no sum.
+__device__ __forceinline__ float times_rstd(float sum, float rstd) { return rstd == 0.0f ? 0.0f : sum * rstd; }
 
 // gamma-weighted sums of the groups from the sums per channel: out[group].
 template <int N, int E>
@@ -427,7 +429,7 @@ __device__ __forceinline__ void weigh(const Place<E, N>& at, const Args& a, cons
         }
         s1 = lanes_sum(s1, l);
         s2 = lanes_sum(s2, l);
-        if (sub == 0 && g == g0) out[g] = make_float2(s1, s2 * rstd[g * a.cg]);
+        if (sub == 0 && g == g0) out[g] = make_float2(s1, times_rstd(s2, rstd[g * a.cg]));
     }
 }
 
@@ -525,7 +527,7 @@ __global__ void __launch_bounds__(N, kMostThreads / N) norm_kernel(const Args a)
         const int g = min(over(i, a.chdiv), at.ng - 1), r = i & (a.chunks - 1);      // (chunks: a power of two, at most 16)
         const float w = (float)pixels_of(a, r) * a.cg;
         const float2 o = a.chunks > 1 ? ld_rank(own + g, r) : own[g];
-        const float mu = lanes_sum(w > 0.0f ? o.x * w : 0.0f, a.chunks) * total;      // (a block without pixels adds nothing, but its lanes take part)
+        const float mu = lanes_sum(w > 0.0f ? o.x * (w * total) : 0.0f, a.chunks);      // (a block without pixels adds nothing, but its lanes take part)
         const float d = o.x - mu;
         const float var = lanes_sum(w > 0.0f ? fmaf(d * d, w * total, o.y * total) : 0.0f, a.chunks);      // (each part's share: less than their sum)
         const float rs = 1.0f / sqrtf(var + a.eps);
@@ -620,7 +622,7 @@ __global__ void __launch_bounds__(kThreads, 6) norm_back_kernel(const Args a)
     for (int i = threadIdx.x; i < at.nch; i += kThreads) {
         float* const to = a.sums + ((size_t)at.img * a.chunks + at.rank) * 2 * a.c + at.ch0 + i;
         to[0] = sums[i];
-        to[a.c] = sums[at.nch + i] * rstd[i];
+        to[a.c] = times_rstd(sums[at.nch + i], rstd[i]);
     }
     weigh<kThreads, E>(at, a, gamma, rstd, sums, own);
     if (a.chunks > 1) cluster_sync();
@@ -784,8 +786,8 @@ __global__ void __launch_bounds__(kSplitThreads, 4) apply_kernel(const Args a)
         const int g = min(g0, at.ng - 1);
         const float2* const from = reinterpret_cast<const float2*>(a.part) + (size_t)at.img * a.chunks * a.groups + at.span * a.gs + g;
         float s = 0.0f, var = 0.0f;
-        for (int k = sub_; k < a.chunks; k += l) s = fmaf(from[(size_t)k * a.groups].x, (float)pixels_of(a, k) * a.cg, s);
-        const float m = lanes_sum(s, l) / total;
+        for (int k = sub_; k < a.chunks; k += l) s = fmaf(from[(size_t)k * a.groups].x, (float)pixels_of(a, k) * a.cg / total, s);
+        const float m = lanes_sum(s, l);
         for (int k = sub_; k < a.chunks; k += l) {
             const float2 o = from[(size_t)k * a.groups];
             var += fmaf((o.x - m) * (o.x - m), (float)pixels_of(a, k) * a.cg / total, o.y / total);      // (each chunk's share: less than their sum)
@@ -894,7 +896,7 @@ __global__ void __launch_bounds__(kSplitThreads, 3) back_stats_kernel(const Args
     float* const to = a.sums + ((size_t)at.img * a.chunks + at.rank) * 2 * a.c + at.ch0;
     for (int i = threadIdx.x; i < at.nch; i += kSplitThreads) {
         to[i] = sums[i];
-        to[a.c + i] = sums[at.nch + i] * rstd[i];
+        to[a.c + i] = times_rstd(sums[at.nch + i], rstd[i]);
     }
     weigh<kSplitThreads, E>(at, a, gamma, rstd, sums, reinterpret_cast<float2*>(a.part) + ((size_t)at.img * a.chunks + at.rank) * a.groups + at.span * a.gs);
 }

@@ -1,4 +1,5 @@
-"""Group norm at the edges of its ranges: clusters with blocks that have no pixels; chains of calls through the same buffers; SiLU far below 0; the most channels."""
+"""Group norm at the edges of its ranges: clusters with blocks that have no pixels; chains of calls through the same buffers; SiLU far below 0; the most
+channels; values near the end of fp32."""
 import numpy as np
 import pytest
 
@@ -116,3 +117,26 @@ def test_silu_far_below_zero(alcs, shape, dtype):
 @pytest.mark.parametrize("dtype,act", [("f32", "none"), ("bf16", "silu")])
 def test_the_most_channels(alcs, shape, dtype, act):
     norm.test_forward_and_backward(alcs, shape, dtype, act)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 30, 30, 64, 8), (2, 3, 3, 35, 5), (2, 56, 56, 64, 2), (1, 448, 448, 32, 8), (1, 5, 4, 3001, 1), (2, 7, 7, 512, 1), (1, 1, 1, 64, 16),
+                                   (3, 17, 23, 150, 30), (1, 130, 90, 1031, 1)], ids=lambda s: "x".join(map(str, s)))
+def test_values_whose_sums_are_beyond_fp32(alcs, shape, dtype):
+    """All values of an image 2^100, 10^36 or 2^126: y is act(beta), the mean the value.  Then both signs of them: squared distances are no numbers of fp32, rstd is 0."""
+    import torch
+    n, h, w, c, groups = shape
+    _, dy, gamma, beta = norm._inputs(9, n, h * w, c, dtype, alcs)
+    t = dy.dtype
+    for value in (2.0 ** 100, 1e36, 2.0 ** 126):
+        x = torch.full_like(dy, value)
+        k = norm.Norm(alcs, x, shape, dtype, "none", 1e-5, gamma, beta)
+        assert torch.equal(k.forward(), beta.to(t).expand_as(x))
+        v = x.flatten()[0].double()
+        assert ((k.mean.double() / v - 1).abs() <= D * U).all() and torch.isfinite(k.rstd).all()
+        if h * w * c // groups < 2:
+            continue
+        sign = torch.where(torch.arange(x.numel(), device="cuda") % 2 == 0, 1, -1).view(x.shape)
+        k = norm.Norm(alcs, x * sign, shape, dtype, "none", 1e-5, gamma, beta)
+        assert torch.equal(k.forward(), beta.to(t).expand_as(x)) and (k.rstd == 0).all()
+        assert (k.backward(dy) == 0).all() and (k.dgamma == 0).all() and torch.isfinite(k.dbeta).all()
