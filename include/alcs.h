@@ -451,17 +451,19 @@ ALCS_API int alcs_spconv2d_plan(const alcs_packed* w, int n, int cin, int h, int
 /* ---------------------------------------------------------------------------------------------
  * Group norm with an activation, channels last (device).
  *
- * The layer between two pointwise layers, for inference and for the fine-tuning that follows pruning.  The `c` channels are
+ * The layer between two pointwise layers that keep their activations channels last, as alcs_mx4_product does, for inference and for training.  (The
+ * pruned layers above keep theirs [n][c][h*wd]: next to them x and y are to be transposed by the caller.)  The `c` channels are
  * `groups` groups of c / groups neighbours; over the pixels and channels of a group of an image
  *     mu = mean x,  var = mean (x - mu)^2,  rstd = 1 / sqrt(var + eps),  xh = (x - mu) * rstd,
  *     z = gamma[channel] * xh + beta[channel],  y = act(z),  act the identity, ALCS_RELU or ALCS_SILU (flags).
  * x and y are device [n][h*wd][c] (NHWC), contiguous, of type dt, aligned to their element size; y may be x itself, but not
  * overlap it otherwise.  gamma and beta are device fp32 [c] or NULL (1 and 0); mean and rstd receive mu and rstd, device fp32
- * [n][groups], or are NULL.  Statistics and everything up to the rounding of y are fp32; the variance comes from
+ * [n][groups], or are NULL.  Statistics and everything up to the rounding of y are held in fp32, with one rounding of y at the end; SiLU's exponential and quotient, and
+ * the steps of a running mean, are the hardware's approximations, good to 2^-22 or so.  The variance comes from
  * running means and differences of means, so that a mean far from 0 costs no accuracy but its own rounding to fp32.  An infinity
  * or NaN in x makes its group of its image NaN.  Distances from the mean whose squares are beyond fp32 (1.8e19 and more) give an rstd of 0, and so
  * y = act(beta), dx = 0 and dgamma = 0; x is at most 2^126 in magnitude for that.  ReLU turns NaN into 0, as in the convolutions.  SiLU and its slope for z below -43
- * (a beta of -FLT_MAX or -infinity as a mask) are what they are at -43, -9.3e-18, instead of less.
+ * (a beta of -FLT_MAX or -infinity as a mask) are what they are at -43, -9.3e-18, and do not go on to 0.
  *
  * alcs_group_norm_backward: for the derivative dy of a loss by y, with dz = dy * act'(z) (act' of ReLU at 0 is 0) and t = gamma * dz,
  *     dbeta = sum dz,  dgamma = sum dz * xh  (over images and pixels),
@@ -469,15 +471,16 @@ ALCS_API int alcs_spconv2d_plan(const alcs_packed* w, int n, int cin, int h, int
  * mean and rstd are what alcs_group_norm stored for the same x; dy and dx are like x, dx may be dy or x itself; dgamma and
  * dbeta are device fp32 [c] or NULL, and are overwritten.  The order of all sums is fixed: the same call gives the same bits.
  *
- * workspace: device memory of at least alcs_group_norm_workspace() bytes, 16-byte aligned, for either call (the forward
- * pass needs it where a group's part of an image is spread over more thread blocks than can exchange sums directly; NULL and 0 where
- * that function says 0).  Its content matters only within a call; calls that may overlap on the GPU need one each, and so do
+ * workspace: device memory of at least alcs_group_norm_workspace() bytes, 16-byte aligned; that is enough for either call, whatever its activation and
+ * the alignment of its buffers.  The backward pass always needs some.  The forward pass needs it only where a group's part of an image is spread over more
+ * thread blocks than can exchange sums directly: it takes less, NULL and 0 too, and answers INVALID_ARG where that is not enough.  Its content matters only within a call; calls that may overlap on the GPU need one each, and so do
  * captured graphs that may.
  * All buffers belong to the current device.  One to three kernels on cuda_stream; no allocation, no synchronisation.  n == 0 or
  * h*wd == 0 is a successful no-op, but for dgamma and dbeta, which become 0.
  * Errors: INVALID_ARG (null, misaligned or overlapping buffers, host memory, negative sizes, groups < 1, an eps that is negative or not finite, both
  * activations, workspace too small), SHAPE (c not a multiple of groups, h*wd or n*c of 2^30 and more, c above 65536),
- * UNSUPPORTED (more than 8192 channels per group), STATE (memory of another device), ALLOC (host), CUDA.
+ * UNSUPPORTED (more than 8192 channels per group), STATE (memory of another device), ALLOC (host), CUDA (also from a context that has part of a B200's
+ * SMs only, where no cluster of 16 blocks with up to 200 KB of shared memory each fits; a whole one holds seven at once).
  * ------------------------------------------------------------------------------------------- */
 ALCS_API size_t alcs_group_norm_workspace(int n, int h, int wd, int c, int groups, alcs_dtype dt);
 ALCS_API int alcs_group_norm(const void* x, void* y, int n, int h, int wd, int c, int groups, const float* gamma, const float* beta,

@@ -30,13 +30,13 @@ inline size_t elt_bytes(alcs_dtype dt) { return dt == ALCS_F32 ? 4 : 2; }
 inline bool known_type(alcs_dtype dt) { return dt == ALCS_F32 || dt == ALCS_F16 || dt == ALCS_BF16; }
 inline long long up_div(long long a, long long b) { return (a + b - 1) / b; }
 
-// A buffer of a call.  `alias`: index of the one buffer that a written one may be (the same start), -1: none, or -2: any.
+// A buffer of a call.
 struct Buffer {
     const void* p;
     size_t bytes, align;
     bool written;
     bool optional;       // may be null
-    unsigned may_be;     // bit i: may start where buffer i starts, and only there overlap it
+    unsigned may_be;     // bit i: may start where buffer i does; any other overlap of a written buffer with another is refused
 };
 
 // Null, misaligned or overlapping buffers; then memory that is not the current device's.

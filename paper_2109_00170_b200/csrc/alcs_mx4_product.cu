@@ -12,7 +12,7 @@
 // What bounds it, measured with 16384x4096x4096 (bf16): the number of copies, about 117 cycles each whatever their size (2 KB at a time 341 us, 8 KB 172,
 // 16 KB 129); the instructions of the one thread that issues the tensor cores' (160 us before their descriptors came down to an addition); then both and
 // what is in flight, three stages of 51 KB: 1070 cycles per stage, 512 of them the tensor cores'.  Tiles of 256 x 256 by pairs of blocks (cta_group::2) fetch a
-// third less and were slower, 177 us: the hand-shakes of a stage take longer than it.  Few columns: the outputs' way to memory.
+// third less and were slower where one block per tile took 160 us, 177: the hand-shakes of a stage took longer than it.  Few columns: the outputs' way to memory.
 // A block has sixteen warps for the epilogue (32 rows x 32 columns of an accumulator each; with eight, 200704x64x256 took 32 us and not 29), one that copies,
 // one that multiplies.  Blocks stay and walk over the tiles.  An accumulator has 128 columns, a tile one or two of the three; the epilogue takes them into
 // registers before it works on them, so that the next tile starts at once.

@@ -10,16 +10,16 @@
 // of a pixel where that is possible: whole sectors of memory) of one image; its pixels are shared out to the blocks of a cluster, and a block holds its
 // share in shared memory, which cp.async fills without holding registers.  A thread keeps to its channels.  Sums go through shared memory, in a fixed
 // order, and between the cluster's blocks through distributed shared memory.  What it costs over a copy is the sums: all blocks of an SM tend to be at them
-// at the same time, with memory idle (64 images of 56x56x128, bf16: 29.4 us among other calls; a copy of them 22.5; the same
+// at the same time, with memory idle (64 images of 56x56x128, bf16: 29.7 us among other calls; a copy of them 22.5; the same
 // kernel without the sums 24.6; floor 15.7 at 6.5 TB/s).
 //
 // Two passes: sums of chunks of pixels, then the outputs from a second reading, which L2 serves as far as it holds x (and dy).  For spans that do
 // not fit a cluster, and for large calls of the backward pass.  Every thread keeps 8 loads (4 of x and dy each) on their way to slots of its own in
 // shared memory: with as many registers instead, a third of the bytes were in flight (backward of 64 images of 56x56x256, SiLU: 143 us, then 105;
-// 46 and 51 us for the passes now).
+// 95 now, 47 and 52 us for the passes by themselves, with cold caches).
 //
 // The variance has no cancellation: a thread takes its values one by one into a running mean and sum of squared distances, and these are united by
-// M2 = M2_a + M2_b + n_a n_b / n (mean_a - mean_b)^2.  A mean of means is a sum of each one's share, so that no sum is larger than the values.  All of it in fp32.
+// M2 = M2_a + M2_b + n_a n_b / n (mean_a - mean_b)^2.  A mean of means is a sum of each one's share, so that no sum is larger than the values.  All of it is held in fp32.
 #include <algorithm>
 #include <cmath>
 #include <mutex>
