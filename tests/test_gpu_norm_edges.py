@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 import test_gpu_norm as norm
-from dense_util import D, HALF, TINY, U, back_bounds, f64, norm_bound
+from dense_util import D, HALF, TINY, U, back_bounds, f64, norm_bound, types
 from oracle import dense
 
 pytestmark = pytest.mark.gpu
@@ -140,3 +140,55 @@ def test_values_whose_sums_are_beyond_fp32(alcs, shape, dtype):
         k = norm.Norm(alcs, x * sign, shape, dtype, "none", 1e-5, gamma, beta)
         assert torch.equal(k.forward(), beta.to(t).expand_as(x)) and (k.rstd == 0).all()
         assert (k.backward(dy) == 0).all() and (k.dgamma == 0).all() and torch.isfinite(k.dbeta).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,c", [(600, 250), (600, 256), (3, 96)])
+def test_a_pruned_layer_behind_a_norm_in_place(alcs, n, c, dtype):
+    """Images of one pixel are channels last and channels first at once: a norm in place and the pruned layer that reads it, 30 times over in one captured graph through the
+    same buffer, against calls that have the GPU to themselves."""
+    import torch
+    cout, g, groups, links = 64, 4, 2, 30
+    dt, t = types(alcs)[dtype]
+    r = np.random.default_rng(n + c)
+    mask = (r.random((cout // g, c)) < 0.3).astype(np.uint8)
+    w = torch.from_numpy(r.normal(size=(cout, c)).astype(np.float32) / 8).to(t)
+    host = w.view(torch.uint16).numpy() if dtype == "bf16" else w.numpy()
+    packed = alcs.alcs_packed_upload(alcs.alcs_pack(host, mask, g, bf16=dtype == "bf16"), 0)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(n)
+    xs = torch.randn(links, n, 1, c, generator=gen, device="cuda").to(t)
+    gamma, x = 1 + 0.3 * torch.randn(c, generator=gen, device="cuda"), torch.empty(n, 1, c, device="cuda", dtype=t)
+    size = alcs.alcs_group_norm_workspace(n, 1, 1, c, groups, dt)
+    ws, ys = torch.empty(size, device="cuda", dtype=torch.uint8), torch.empty(links, n, cout, 1, device="cuda", dtype=t)
+
+    def run(stream, wait):
+        for i in range(links):
+            x.copy_(xs[i])
+            for k in range(2):
+                alcs.alcs_group_norm(x, x, n, 1, 1, c, groups, gamma, None, 1e-5, alcs.ALCS_RELU if k else 0, dt, None, None, ws, size, stream)
+                if wait:
+                    torch.cuda.synchronize()
+                alcs.alcs_spconv1x1(packed, x, ys[i], n, 1, 1, None, 0, stream)
+                if wait:
+                    torch.cuda.synchronize()
+
+    run(torch.cuda.current_stream(), True)
+    want = ys.clone()
+    assert torch.isfinite(want).all() and want.abs().max() > 0
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        run(stream, False)
+    for _ in range(10):
+        ys.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(ys, want)
+    last = dense.group_norm(f64(xs[-1]), groups, f64(gamma))["y"].reshape(n, 1, c)
+    if dtype == "f32":
+        # The last link against the definitions.  A norm is off by D u |gamma| (|xh| + M), 64 x 2^-24 x 2 x 10 = 8e-5 with gamma below 2 and values below 5; the first one's
+        # error goes through the second, whose rstd is about 1; a sum of 128 products by 128 u |W| |z|, 8e-6: less than 4e-4 (1 + |z|) |W|.
+        z = dense.group_norm(last, groups, f64(gamma), act="relu")["y"].reshape(n, c)
+        full = f64(w) * np.repeat(mask, g, 0)
+        assert (np.abs(f64(ys[-1])[:, :, 0] - z @ full.T) <= 4e-4 * (1 + np.abs(z)) @ np.abs(full).T).all()
